@@ -280,6 +280,146 @@ hs2_status hs2_select_from_scores(const hs2_dims* dims, const float* scores, con
 #define HS2_STREAM_PROBE_SINK_WORDS 4096
 hs2_status hs2_stream_read_probe(const void* src, size_t bytes, int32_t mode, uint32_t* sink, void* stream);
 
+/* ---------------------------------------------------------------- paged KV cache
+ * A cache whose sequences hold pages of a pool instead of one range of memory
+ * each, with the decode attention of the model's other layers over it: full
+ * attention without a selection, and sliding-window attention (the
+ * self-decoder is "a hybrid of full attention and SWA layers", Sec.
+ * "HySparse2 Overview"; its SWA layers carry per-head sinks and output gates,
+ * Sec. "Experimental Setup").  The paper does not say how a cache is stored;
+ * pages, their tables and counts are this library's.
+ *
+ *   pool    K, V: element (p, g, s, d) of page p, KV head g, slot s at
+ *           p*kv_stride_p + g*kv_stride_h + s*kv_stride_t + d (bf16, or E4M3
+ *           bytes for the _fp8 entry points with scales as above; K and V
+ *           share this layout; each token row is contiguous).  Several
+ *           layers' pools may share one table.
+ *   table   [batch, max_pages] int32 (device): entry (b, j) is the page of
+ *           sequence b's tokens j*page .. j*page + page - 1.  Entries outside
+ *           [0, n_pages) are no page: reads skip their tokens (as if no query
+ *           saw them), writes drop them.
+ *   len     [batch] int32 (device), as for the calls above, clamped to
+ *           [0, page * max_pages]; the new tokens are the last n_queries.
+ *   refs    [n_pages] int32 (device): how many table entries name a page
+ *           (and whoever else holds it); a page with refs <= 0 is free.
+ * Every call of this part is asynchronous on `stream` and can be captured
+ * into a graph; `workspace` may be shared by calls that are ordered.         */
+typedef struct hs2_paged_dims {
+  int32_t batch;       /* B >= 1: sequences (rows of the table)                  */
+  int32_t n_queries;   /* C: new tokens per sequence, 1 .. 16 (attention)        */
+  int32_t n_q_heads;   /* Hq, Hkv, G, C: limits as in hs2_dims                   */
+  int32_t n_kv_heads;
+  int32_t head_dim;    /* D: 128 or 256 (else HS2_ERR_UNSUPPORTED)               */
+  int32_t page;        /* tokens per page: 16, 32, 64, 128 or 256                */
+  int32_t n_pages;     /* pages of the pool, 1 .. 2^24                           */
+  int32_t max_pages;   /* table entries per sequence; page * max_pages <= 2^27   */
+  int64_t kv_stride_p; /* elements; multiple of 8 (16 for E4M3)                  */
+  int64_t kv_stride_h; /* elements; multiple of 8 (16)                           */
+  int64_t kv_stride_t; /* elements; >= head_dim, multiple of 8 (16), <= 2^24     */
+  float scale;         /* softmax scale; <= 0 selects 1/sqrt(head_dim)           */
+} hs2_paged_dims;
+
+/* Bytes of device workspace that every call below needs for these dims.
+ * Host-only.  Returns 0 if the dims are invalid.                             */
+size_t hs2_paged_workspace_bytes(const hs2_paged_dims* dims);
+
+/* Attention of the new tokens over every token of their sequence: query c at
+ * pos = len[b] - C + c sees the tokens [0, pos].
+ *   q, out  [B, C, Hq, D] bf16 (fp32 accumulation; a query that sees no token
+ *           gives 0)
+ *   sink, gate  as for hs2_sparse_attn_ex, either may be NULL
+ * What a query does not see does not touch its output, whatever the pool
+ * holds there (slots behind a sequence's end, pages of others, NaN).         */
+hs2_status hs2_paged_attn(const hs2_paged_dims* dims, const uint16_t* q, const uint16_t* K, const uint16_t* V,
+                          const int32_t* table, const int32_t* len, const float* sink, const uint16_t* gate,
+                          uint16_t* out, void* workspace, size_t workspace_bytes, void* stream);
+hs2_status hs2_paged_attn_fp8(const hs2_paged_dims* dims, const uint16_t* q, const uint8_t* K8, const uint8_t* V8,
+                              const float* k_scale, const float* v_scale, const int32_t* table, const int32_t* len,
+                              const float* sink, const uint16_t* gate, uint16_t* out, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* The same with a sliding window and first tokens that stay visible: query c
+ * sees the tokens t <= pos with t > pos - window or t < first.
+ *   window  1 .. 2^27, first  0 .. 2^27 (HS2_ERR_SHAPE)                        */
+hs2_status hs2_paged_window_attn(const hs2_paged_dims* dims, const uint16_t* q, const uint16_t* K, const uint16_t* V,
+                                 const int32_t* table, const int32_t* len, int32_t window, int32_t first,
+                                 const float* sink, const uint16_t* gate, uint16_t* out, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+hs2_status hs2_paged_window_attn_fp8(const hs2_paged_dims* dims, const uint16_t* q, const uint8_t* K8,
+                                     const uint8_t* V8, const float* k_scale, const float* v_scale,
+                                     const int32_t* table, const int32_t* len, int32_t window, int32_t first,
+                                     const float* sink, const uint16_t* gate, uint16_t* out, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/* Writes new tokens' K and V rows into their pages.
+ *   k_new, v_new  bf16: row (b, i, g) at b*new_stride_b + i*new_stride_t +
+ *           g*new_stride_h, D contiguous elements (strides multiples of 8,
+ *           pointers 16-byte aligned), i in [0, n_tokens)
+ *   n_tokens  >= 1 (dims->n_queries is not used)
+ *   n_new   [B] int32 (device) or NULL (n_tokens for every sequence): rows
+ *           i < n_new[b] (clamped to [0, n_tokens]) are written, to token
+ *           len[b] - n_new[b] + i; the rows behind them are not read.  Tokens
+ *           below 0 are dropped.
+ * bf16 rows keep their bits.  E4M3: the value nearest to x / scale[g] (ties to
+ * even), beyond +-448 saturated, NaN stays NaN.  Two sequences that write one
+ * slot of one page leave either's row (16 bytes at a time): give a shared
+ * page its own copy first (hs2_pages_reorder does).                          */
+hs2_status hs2_paged_append(const hs2_paged_dims* dims, const uint16_t* k_new, const uint16_t* v_new,
+                            int64_t new_stride_b, int64_t new_stride_t, int64_t new_stride_h, int32_t n_tokens,
+                            const int32_t* n_new, const int32_t* table, const int32_t* len, uint16_t* K, uint16_t* V,
+                            void* stream);
+hs2_status hs2_paged_append_fp8(const hs2_paged_dims* dims, const uint16_t* k_new, const uint16_t* v_new,
+                                int64_t new_stride_b, int64_t new_stride_t, int64_t new_stride_h, int32_t n_tokens,
+                                const int32_t* n_new, const float* k_scale, const float* v_scale,
+                                const int32_t* table, const int32_t* len, uint8_t* K8, uint8_t* V8, void* stream);
+
+/* Pages for longer sequences: row b gets free pages (lowest first, rows in
+ * order) behind its last entry until it holds ceil(len[b] / page).
+ *   table_out, refs_out  the new table and counts; each may be the input itself
+ *   counts  [2] int32 (device, written): pages given; pages wanted that the
+ *           pool did not have (their entries stay as they were)                */
+hs2_status hs2_pages_extend(const hs2_paged_dims* dims, const int32_t* table, const int32_t* len,
+                            const int32_t* refs, int32_t* table_out, int32_t* refs_out, int32_t* counts,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* Every row takes over the tokens of its parent row: forks (two rows of one
+ * parent), beams, permutations and frees (a row outside [0, batch) as parent)
+ * in one step.
+ *   parent  [B] int32 (device)
+ * One child of each parent, its heir (the parent row itself if it stays, else
+ * the lowest), takes over the parent's entries as they are.  The others share
+ * the full pages (refs + 1), and if the last page is not full they get a free
+ * page for it (lowest first, rows in order; pages freed by this call are not
+ * among them), whose tokens a move tells to copy.  Rows that are nobody's
+ * parent give up their entries (refs - 1).  A child that finds no free page is
+ * cut to its full pages.
+ *   table_out [B, max_pages], len_out [B]  the new table and lengths; not the
+ *           inputs.  refs_out may be refs itself
+ *   moves   [max_moves, 3] int32 (device): (from page, to page, tokens) of each
+ *           copy; max_moves >= B; rows from counts[0] on are left as they were
+ *   counts  [2] int32 (device, written): moves; children that were cut       */
+hs2_status hs2_pages_reorder(const hs2_paged_dims* dims, const int32_t* parent, const int32_t* table,
+                             const int32_t* len, const int32_t* refs, int32_t* table_out, int32_t* len_out,
+                             int32_t* refs_out, int32_t* moves, int32_t max_moves, int32_t* counts, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Packs the pages in use to the front of the pool: the n-th used page behind
+ * them moves to the n-th free page among them.
+ *   table_out, refs_out  the new table and counts; each may be the input itself
+ *   moves   [max_moves, 3], max_moves >= n_pages / 2; as above (tokens = page)
+ *   counts  [2] int32 (device, written): moves; pages in use                  */
+hs2_status hs2_pages_compact(const hs2_paged_dims* dims, const int32_t* table, const int32_t* refs,
+                             int32_t* table_out, int32_t* refs_out, int32_t* moves, int32_t max_moves,
+                             int32_t* counts, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Copies within one layer's pool: the first `tokens` slots of every KV head of
+ * page `from` to page `to`, for the first n_moves[0] (device, clamped to
+ * [0, max_moves]) of the moves.  elem_bytes: 2 (bf16) or 1 (E4M3).  Moves from
+ * or to a page outside the pool are skipped; no page may be a move's target
+ * and another's source or target (those of the calls above never are).       */
+hs2_status hs2_pages_copy(const hs2_paged_dims* dims, const int32_t* moves, const int32_t* n_moves,
+                          int32_t max_moves, int32_t elem_bytes, void* K, void* V, void* stream);
+
 /* Static description of a status code. */
 const char* hs2_status_string(int32_t status);
 

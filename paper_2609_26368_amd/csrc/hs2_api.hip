@@ -393,9 +393,11 @@ bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 // ---------------------------------------------------------------- timing
 enum KernelKind { KK_FA = 0, KK_COMBINE, KK_POOL, KK_POOL_LOGITS, KK_SCORE_SELECT, KK_SEL_INIT, KK_SEL_HIST, KK_SELECT,
-                  KK_BLOCK_SELECT, KK_SA, KK_SA_COMBINE, KK_COUNT };
+                  KK_BLOCK_SELECT, KK_SA, KK_SA_COMBINE, KK_PAGED_ATTN, KK_PAGED_MERGE, KK_PAGED_APPEND, KK_PAGES_SCAN,
+                  KK_PAGES_ROWS, KK_PAGES_LIST, KK_PAGES_COPY, KK_COUNT };
 const char* kKindNames[KK_COUNT] = {"fa_split", "fa_combine", "pool_scores", "pool_logits", "score_select", "sel_init", "sel_hist",
-                                    "select", "block_select", "sa_split", "sa_combine"};
+                                    "select", "block_select", "sa_split", "sa_combine", "paged_attn", "paged_merge",
+                                    "paged_append", "pages_scan", "pages_rows", "pages_list", "pages_copy"};
 constexpr int kMaxTimed = 16384;
 struct Timing {
   bool on = false;
@@ -960,6 +962,317 @@ hs2_status hs2_stream_read_probe(const void* src, size_t bytes, int32_t mode, ui
   hipStream_t s = (hipStream_t)stream;
   const hipError_t e = launch_stream_probe(src, (int64_t)(bytes / 16), mode, sink, s);
   if (e != hipSuccess) return fail(HS2_ERR_HIP, "stream probe launch: %s", hipGetErrorString(e));
+  return HS2_OK;
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- paged cache
+namespace {
+
+constexpr int kMaxPages = 1 << 24;  // of a pool: their chunks' prefix sums sit in LDS
+
+// kv8: E4M3 strides
+hs2_status check_paged(const hs2_paged_dims* d, bool kv8) {
+  if (!d) return fail(HS2_ERR_NULL, "dims is NULL");
+  if (d->page < 16 || d->page > 256 || (d->page & (d->page - 1)))
+    return fail(HS2_ERR_SHAPE, "page must be a power of two in [16, 256] (got %d)", d->page);
+  if (d->n_pages < 1 || d->n_pages > kMaxPages) return fail(HS2_ERR_SHAPE, "n_pages must be in [1, 2^24]");
+  if (d->max_pages < 1 || (int64_t)d->max_pages * d->page > kMaxLen)
+    return fail(HS2_ERR_SHAPE, "max_pages must be >= 1 and page * max_pages at most 2^27");
+  if (d->kv_stride_p < 0 || d->kv_stride_p % 8) return fail(HS2_ERR_ALIGN, "kv_stride_p must be a non-negative multiple of 8 elements");
+  hs2_dims rest{d->batch, d->n_queries, d->n_q_heads, d->n_kv_heads, d->head_dim, d->page * d->max_pages,
+                d->kv_stride_p, d->kv_stride_h, d->kv_stride_t, d->scale};
+  const hs2_status st = check_dims(&rest);
+  if (st != HS2_OK) return st;
+  if (kv8 && (d->kv_stride_p % 16 || d->kv_stride_h % 16 || d->kv_stride_t % 16))
+    return fail(HS2_ERR_ALIGN, "FP8 pool strides must be multiples of 16 elements");
+  return HS2_OK;
+}
+
+PagedPool paged_pool(const hs2_paged_dims* d, const void* K, const void* V, const int32_t* table, const int32_t* len,
+                     int esz) {
+  PagedPool p{};
+  p.K = (unsigned char*)const_cast<void*>(K);
+  p.V = (unsigned char*)const_cast<void*>(V);
+  p.stride_p = d->kv_stride_p * esz;
+  p.stride_h = d->kv_stride_h * esz;
+  p.stride_t = d->kv_stride_t * esz;
+  p.table = table;
+  p.len = len;
+  p.B = d->batch;
+  p.Hkv = d->n_kv_heads;
+  p.hd = d->head_dim;
+  p.page = d->page;
+  p.page_shift = ilog2(d->page);
+  p.n_pages = d->n_pages;
+  p.max_pages = d->max_pages;
+  return p;
+}
+
+// workspace of the page operators
+struct PagesPlan {
+  int n_chunks;
+  size_t off_chunk_n, off_list, off_need, off_have, bytes;
+};
+PagesPlan pages_plan(const hs2_paged_dims* d) {
+  PagesPlan p;
+  p.n_chunks = (int)cdiv(d->n_pages, PAGES_CHUNK);
+  size_t cur = 0;
+  p.off_chunk_n = carve(cur, sizeof(int32_t) * p.n_chunks);
+  p.off_list = carve(cur, sizeof(int32_t) * (size_t)p.n_chunks * PAGES_CHUNK);
+  p.off_need = carve(cur, sizeof(int32_t) * d->batch);
+  p.off_have = carve(cur, sizeof(int32_t) * d->batch);
+  p.bytes = (size_t)round_up((int64_t)cur, kAlign);
+  return p;
+}
+
+// window 0: every token
+hs2_status paged_attn_impl(const hs2_paged_dims* d, const uint16_t* q, const void* K, const void* V, bool kv8,
+                           const float* k_scale, const float* v_scale, const int32_t* table, const int32_t* len,
+                           int32_t window, int32_t first, const float* sink, const uint16_t* gate, uint16_t* out,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  hs2_status st = check_paged(d, kv8);
+  if (st != HS2_OK) return st;
+  if (!q || !K || !V || !table || !len || !out || !workspace)
+    return fail(HS2_ERR_NULL, "q, K, V, table, len, out and workspace are required");
+  if (kv8 && (!k_scale || !v_scale)) return fail(HS2_ERR_NULL, "k_scale and v_scale are required for an FP8 cache");
+  if (!aligned(q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(out, 16) || !aligned(table, 4) ||
+      !aligned(len, 4) || !aligned(workspace, kAlign) || (sink && !aligned(sink, 4)) || (gate && !aligned(gate, 8)) ||
+      (kv8 && (!aligned(k_scale, 4) || !aligned(v_scale, 4))))
+    return fail(HS2_ERR_ALIGN,
+                "q/K/V/out need 16-byte, workspace 256-byte, gate 8-byte, table/len/sink/scales 4-byte alignment");
+  const size_t need = hs2_paged_workspace_bytes(d);
+  if (workspace_bytes < need)
+    return fail(HS2_ERR_WORKSPACE, "workspace %zu bytes < %zu required", workspace_bytes, need);
+  if ((st = ensure_device_init(nullptr)) != HS2_OK) return st;
+  PagedAttnArgs a{};
+  a.p = paged_pool(d, K, V, table, len, kv8 ? 1 : 2);
+  a.q = q;
+  a.out = out;
+  const double scale = d->scale > 0.f ? (double)d->scale : 1.0 / std::sqrt((double)d->head_dim);
+  a.c2 = (float)(scale * 1.4426950408889634);
+  a.C = d->n_queries;
+  a.Hq = d->n_q_heads;
+  a.G = d->n_q_heads / d->n_kv_heads;
+  a.Gp = next_pow2(a.G);
+  a.window = window;
+  a.first = first;
+  a.k_scale = k_scale;
+  a.v_scale = v_scale;
+  a.sink = sink;
+  a.gate = gate;
+  HS2_TRY_LAUNCH(KK_PAGED_ATTN, (hipStream_t)stream, launch_paged_attn(a, (hipStream_t)stream));
+  return HS2_OK;
+}
+
+hs2_status check_window(int32_t window, int32_t first) {
+  if (window < 1 || window > kMaxLen) return fail(HS2_ERR_SHAPE, "window must be in [1, 2^27] (got %d)", window);
+  if (first < 0 || first > kMaxLen) return fail(HS2_ERR_SHAPE, "first must be in [0, 2^27] (got %d)", first);
+  return HS2_OK;
+}
+
+hs2_status paged_append_impl(const hs2_paged_dims* d, const uint16_t* k_new, const uint16_t* v_new, int64_t stride_b,
+                             int64_t stride_t, int64_t stride_h, int32_t n_tokens, const int32_t* n_new, bool kv8,
+                             const float* k_scale, const float* v_scale, const int32_t* table, const int32_t* len,
+                             void* K, void* V, void* stream) {
+  hs2_status st = check_paged(d, kv8);
+  if (st != HS2_OK) return st;
+  if (n_tokens < 1 || (int64_t)n_tokens * d->n_kv_heads > (1 << 27))
+    return fail(HS2_ERR_SHAPE, "n_tokens must be >= 1 and n_tokens * n_kv_heads at most 2^27 (got %d)", n_tokens);
+  if (!k_new || !v_new || !table || !len || !K || !V)
+    return fail(HS2_ERR_NULL, "k_new, v_new, table, len, K and V are required");
+  if (kv8 && (!k_scale || !v_scale)) return fail(HS2_ERR_NULL, "k_scale and v_scale are required for an FP8 cache");
+  if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(table, 4) ||
+      !aligned(len, 4) || (n_new && !aligned(n_new, 4)) || (kv8 && (!aligned(k_scale, 4) || !aligned(v_scale, 4))))
+    return fail(HS2_ERR_ALIGN, "k_new/v_new/K/V need 16-byte, table/len/n_new/scales 4-byte alignment");
+  if (stride_b < 0 || stride_t < 0 || stride_h < 0 || stride_b % 8 || stride_t % 8 || stride_h % 8)
+    return fail(HS2_ERR_ALIGN, "strides of k_new and v_new must be non-negative multiples of 8 elements");
+  if ((st = ensure_device_init(nullptr)) != HS2_OK) return st;
+  PagedAppendArgs a{};
+  a.p = paged_pool(d, K, V, table, len, kv8 ? 1 : 2);
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.stride_b = stride_b;
+  a.stride_t = stride_t;
+  a.stride_h = stride_h;
+  a.n_tokens = n_tokens;
+  a.n_new = n_new;
+  a.k_scale = k_scale;
+  a.v_scale = v_scale;
+  HS2_TRY_LAUNCH(KK_PAGED_APPEND, (hipStream_t)stream, launch_paged_append(a, (hipStream_t)stream));
+  return HS2_OK;
+}
+
+// what the page operators check and fill alike
+hs2_status pages_args(const hs2_paged_dims* d, const int32_t* table, const int32_t* refs, int32_t* table_out,
+                      int32_t* refs_out, int32_t* counts, void* workspace, size_t workspace_bytes, PagesArgs& a) {
+  hs2_status st = check_paged(d, false);
+  if (st != HS2_OK) return st;
+  if (!table || !refs || !table_out || !refs_out || !counts || !workspace)
+    return fail(HS2_ERR_NULL, "table, refs, table_out, refs_out, counts and workspace are required");
+  if (!aligned(table, 4) || !aligned(refs, 4) || !aligned(table_out, 4) || !aligned(refs_out, 4) ||
+      !aligned(counts, 4) || !aligned(workspace, kAlign))
+    return fail(HS2_ERR_ALIGN, "tables, counts need 4-byte, workspace 256-byte alignment");
+  const PagesPlan p = pages_plan(d);
+  if (workspace_bytes < p.bytes)
+    return fail(HS2_ERR_WORKSPACE, "workspace %zu bytes < %zu required", workspace_bytes, p.bytes);
+  a = PagesArgs{};
+  a.table = table;
+  a.refs = refs;
+  a.table_out = table_out;
+  a.refs_out = refs_out;
+  a.counts = counts;
+  a.B = d->batch;
+  a.page = d->page;
+  a.n_pages = d->n_pages;
+  a.max_pages = d->max_pages;
+  a.n_chunks = p.n_chunks;
+  char* ws = (char*)workspace;
+  a.chunk_n = (int32_t*)(ws + p.off_chunk_n);
+  a.list = (int32_t*)(ws + p.off_list);
+  a.row_need = (int32_t*)(ws + p.off_need);
+  a.row_have = (int32_t*)(ws + p.off_have);
+  return HS2_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t hs2_paged_workspace_bytes(const hs2_paged_dims* d) {
+  if (check_paged(d, false) != HS2_OK) return 0;
+  return pages_plan(d).bytes;
+}
+
+hs2_status hs2_paged_attn(const hs2_paged_dims* d, const uint16_t* q, const uint16_t* K, const uint16_t* V,
+                          const int32_t* table, const int32_t* len, const float* sink, const uint16_t* gate,
+                          uint16_t* out, void* workspace, size_t workspace_bytes, void* stream) {
+  return paged_attn_impl(d, q, K, V, false, nullptr, nullptr, table, len, 0, 0, sink, gate, out, workspace,
+                         workspace_bytes, stream);
+}
+
+hs2_status hs2_paged_attn_fp8(const hs2_paged_dims* d, const uint16_t* q, const uint8_t* K, const uint8_t* V,
+                              const float* k_scale, const float* v_scale, const int32_t* table, const int32_t* len,
+                              const float* sink, const uint16_t* gate, uint16_t* out, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  return paged_attn_impl(d, q, K, V, true, k_scale, v_scale, table, len, 0, 0, sink, gate, out, workspace,
+                         workspace_bytes, stream);
+}
+
+hs2_status hs2_paged_window_attn(const hs2_paged_dims* d, const uint16_t* q, const uint16_t* K, const uint16_t* V,
+                                 const int32_t* table, const int32_t* len, int32_t window, int32_t first,
+                                 const float* sink, const uint16_t* gate, uint16_t* out, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  const hs2_status st = check_window(window, first);
+  if (st != HS2_OK) return st;
+  return paged_attn_impl(d, q, K, V, false, nullptr, nullptr, table, len, window, first, sink, gate, out, workspace,
+                         workspace_bytes, stream);
+}
+
+hs2_status hs2_paged_window_attn_fp8(const hs2_paged_dims* d, const uint16_t* q, const uint8_t* K, const uint8_t* V,
+                                     const float* k_scale, const float* v_scale, const int32_t* table,
+                                     const int32_t* len, int32_t window, int32_t first, const float* sink,
+                                     const uint16_t* gate, uint16_t* out, void* workspace, size_t workspace_bytes,
+                                     void* stream) {
+  const hs2_status st = check_window(window, first);
+  if (st != HS2_OK) return st;
+  return paged_attn_impl(d, q, K, V, true, k_scale, v_scale, table, len, window, first, sink, gate, out, workspace,
+                         workspace_bytes, stream);
+}
+
+hs2_status hs2_paged_append(const hs2_paged_dims* d, const uint16_t* k_new, const uint16_t* v_new,
+                            int64_t new_stride_b, int64_t new_stride_t, int64_t new_stride_h, int32_t n_tokens,
+                            const int32_t* n_new, const int32_t* table, const int32_t* len, uint16_t* K, uint16_t* V,
+                            void* stream) {
+  return paged_append_impl(d, k_new, v_new, new_stride_b, new_stride_t, new_stride_h, n_tokens, n_new, false, nullptr,
+                           nullptr, table, len, K, V, stream);
+}
+
+hs2_status hs2_paged_append_fp8(const hs2_paged_dims* d, const uint16_t* k_new, const uint16_t* v_new,
+                                int64_t new_stride_b, int64_t new_stride_t, int64_t new_stride_h, int32_t n_tokens,
+                                const int32_t* n_new, const float* k_scale, const float* v_scale,
+                                const int32_t* table, const int32_t* len, uint8_t* K, uint8_t* V, void* stream) {
+  return paged_append_impl(d, k_new, v_new, new_stride_b, new_stride_t, new_stride_h, n_tokens, n_new, true, k_scale,
+                           v_scale, table, len, K, V, stream);
+}
+
+hs2_status hs2_pages_extend(const hs2_paged_dims* d, const int32_t* table, const int32_t* len, const int32_t* refs,
+                            int32_t* table_out, int32_t* refs_out, int32_t* counts, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  PagesArgs a;
+  hs2_status st = pages_args(d, table, refs, table_out, refs_out, counts, workspace, workspace_bytes, a);
+  if (st != HS2_OK) return st;
+  if (!len) return fail(HS2_ERR_NULL, "len is required");
+  if (!aligned(len, 4)) return fail(HS2_ERR_ALIGN, "len needs 4-byte alignment");
+  if ((st = ensure_device_init(nullptr)) != HS2_OK) return st;
+  a.len = len;
+  hipStream_t s = (hipStream_t)stream;
+  HS2_TRY_LAUNCH(KK_PAGES_SCAN, s, launch_pages_scan(a, PagesOp::extend, s));
+  HS2_TRY_LAUNCH(KK_PAGES_ROWS, s, launch_pages_extend(a, s));
+  return HS2_OK;
+}
+
+hs2_status hs2_pages_reorder(const hs2_paged_dims* d, const int32_t* parent, const int32_t* table, const int32_t* len,
+                             const int32_t* refs, int32_t* table_out, int32_t* len_out, int32_t* refs_out,
+                             int32_t* moves, int32_t max_moves, int32_t* counts, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  PagesArgs a;
+  hs2_status st = pages_args(d, table, refs, table_out, refs_out, counts, workspace, workspace_bytes, a);
+  if (st != HS2_OK) return st;
+  if (!parent || !len || !len_out || !moves) return fail(HS2_ERR_NULL, "parent, len, len_out and moves are required");
+  if (!aligned(parent, 4) || !aligned(len, 4) || !aligned(len_out, 4) || !aligned(moves, 4))
+    return fail(HS2_ERR_ALIGN, "parent, len, len_out and moves need 4-byte alignment");
+  if (table_out == table || len_out == len) return fail(HS2_ERR_SHAPE, "table_out and len_out must not be the inputs");
+  if (max_moves < d->batch) return fail(HS2_ERR_SHAPE, "max_moves (%d) must be at least batch (%d)", max_moves, d->batch);
+  if ((st = ensure_device_init(nullptr)) != HS2_OK) return st;
+  a.parent = parent;
+  a.len = len;
+  a.len_out = len_out;
+  a.moves = moves;
+  hipStream_t s = (hipStream_t)stream;
+  HS2_TRY_LAUNCH(KK_PAGES_SCAN, s, launch_pages_scan(a, PagesOp::reorder, s));
+  HS2_TRY_LAUNCH(KK_PAGES_ROWS, s, launch_pages_reorder(a, s));
+  return HS2_OK;
+}
+
+hs2_status hs2_pages_compact(const hs2_paged_dims* d, const int32_t* table, const int32_t* refs, int32_t* table_out,
+                             int32_t* refs_out, int32_t* moves, int32_t max_moves, int32_t* counts, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  PagesArgs a;
+  hs2_status st = pages_args(d, table, refs, table_out, refs_out, counts, workspace, workspace_bytes, a);
+  if (st != HS2_OK) return st;
+  if (!moves) return fail(HS2_ERR_NULL, "moves is required");
+  if (!aligned(moves, 4)) return fail(HS2_ERR_ALIGN, "moves needs 4-byte alignment");
+  if (max_moves < d->n_pages / 2)
+    return fail(HS2_ERR_SHAPE, "max_moves (%d) must be at least n_pages / 2 (%d)", max_moves, d->n_pages / 2);
+  if ((st = ensure_device_init(nullptr)) != HS2_OK) return st;
+  a.moves = moves;
+  hipStream_t s = (hipStream_t)stream;
+  HS2_TRY_LAUNCH(KK_PAGES_SCAN, s, launch_pages_scan(a, PagesOp::compact, s));
+  HS2_TRY_LAUNCH(KK_PAGES_LIST, s, launch_pages_list(a, s));
+  HS2_TRY_LAUNCH(KK_PAGES_ROWS, s, launch_pages_compact(a, s));
+  return HS2_OK;
+}
+
+hs2_status hs2_pages_copy(const hs2_paged_dims* d, const int32_t* moves, const int32_t* n_moves, int32_t max_moves,
+                          int32_t elem_bytes, void* K, void* V, void* stream) {
+  if (elem_bytes != 1 && elem_bytes != 2) return fail(HS2_ERR_SHAPE, "elem_bytes must be 1 or 2 (got %d)", elem_bytes);
+  hs2_status st = check_paged(d, elem_bytes == 1);
+  if (st != HS2_OK) return st;
+  if (!moves || !n_moves || !K || !V) return fail(HS2_ERR_NULL, "moves, n_moves, K and V are required");
+  if (!aligned(moves, 4) || !aligned(n_moves, 4) || !aligned(K, 16) || !aligned(V, 16))
+    return fail(HS2_ERR_ALIGN, "K/V need 16-byte, moves/n_moves 4-byte alignment");
+  if (max_moves < 0) return fail(HS2_ERR_SHAPE, "max_moves must be >= 0");
+  if (max_moves == 0) return HS2_OK;
+  if ((st = ensure_device_init(nullptr)) != HS2_OK) return st;
+  PagesCopyArgs a{};
+  a.p = paged_pool(d, K, V, nullptr, nullptr, elem_bytes);
+  a.moves = moves;
+  a.n_moves = n_moves;
+  a.max_moves = max_moves;
+  a.esz = elem_bytes;
+  HS2_TRY_LAUNCH(KK_PAGES_COPY, (hipStream_t)stream, launch_pages_copy(a, (hipStream_t)stream));
   return HS2_OK;
 }
 

@@ -175,4 +175,77 @@ hipError_t launch_sa_unit(const SaArgs& a, int NW, hipStream_t s);
 constexpr int STREAM_PROBE_WORKGROUPS = 4096;
 hipError_t launch_stream_probe(const void* src, int64_t n16, int mode, uint32_t* sink, hipStream_t s);
 
+// ---------------------------------------------------------------- paged cache
+// A pool of pages with the tables of its sequences; strides in bytes.
+struct PagedPool {
+  unsigned char* K;
+  unsigned char* V;
+  int64_t stride_p, stride_h, stride_t;
+  const int32_t* table;  // [B][max_pages]
+  const int32_t* len;    // [B]
+  int B, Hkv, hd, page, page_shift, n_pages, max_pages;
+};
+
+struct PagedAttnArgs {
+  PagedPool p;
+  const uint16_t* q;
+  uint16_t* out;           // [B, C, Hq, hd]
+  float c2;                // softmax scale * log2(e)
+  int C, Hq, G, Gp;
+  int window, first;       // window 0: every token is seen
+  const float* k_scale;    // [Hkv] for an E4M3 pool, else null
+  const float* v_scale;
+  const float* sink;       // [Hq] or null
+  const uint16_t* gate;    // [B, C, Hq, hd] or null
+};
+hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
+
+struct PagedAppendArgs {
+  PagedPool p;
+  const uint16_t* k_new;
+  const uint16_t* v_new;
+  int64_t stride_b, stride_t, stride_h;  // elements
+  int n_tokens;
+  const int32_t* n_new;    // [B] or null
+  const float* k_scale;    // [Hkv] for an E4M3 pool, else null
+  const float* v_scale;
+};
+hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t s);
+
+// Page operators: free (or used) pages are listed in chunks of
+// PAGES_CHUNK pages, one workgroup each.
+constexpr int PAGES_CHUNK = 4096;
+struct PagesArgs {
+  const int32_t* table;
+  const int32_t* len;
+  const int32_t* refs;
+  const int32_t* parent;   // reorder
+  int32_t* table_out;
+  int32_t* len_out;        // reorder
+  int32_t* refs_out;
+  int32_t* moves;          // [][3] reorder, compact
+  int32_t* counts;
+  int B, page, n_pages, max_pages, n_chunks;
+  // workspace
+  int32_t* chunk_n;        // [n_chunks] pages listed of each chunk
+  int32_t* list;           // [n_chunks * PAGES_CHUNK] extend, reorder: the free pages of each chunk in order; compact: what
+                           // becomes of each page
+  int32_t* row_need;       // [B] extend, reorder: pages that the row wants
+  int32_t* row_have;       // [B] extend: entries that it has; reorder: its part (ROW_HEIR, ROW_CHILDLESS)
+};
+enum class PagesOp { extend, reorder, compact };
+hipError_t launch_pages_scan(const PagesArgs& a, PagesOp op, hipStream_t s);  // first launch of each operator
+hipError_t launch_pages_extend(const PagesArgs& a, hipStream_t s);
+hipError_t launch_pages_reorder(const PagesArgs& a, hipStream_t s);
+hipError_t launch_pages_list(const PagesArgs& a, hipStream_t s);     // compact: second launch
+hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t s);  // third
+
+struct PagesCopyArgs {
+  PagedPool p;
+  const int32_t* moves;
+  const int32_t* n_moves;
+  int max_moves, esz;
+};
+hipError_t launch_pages_copy(const PagesCopyArgs& a, hipStream_t s);
+
 }  // namespace hs2

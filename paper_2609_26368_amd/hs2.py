@@ -10,6 +10,7 @@ The library must have been built (``__graft_entry__.build()`` or
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -29,6 +30,9 @@ HS2_ERR_HIP = -6
 EXPORTED = ["hs2_workspace_bytes", "hs2_full_attn_score_select", "hs2_sparse_attn", "hs2_sparse_attn_ex",
             "hs2_full_attn_score_select_fp8", "hs2_sparse_attn_fp8", "hs2_full_attn_score_select_blocks",
             "hs2_select_from_scores", "hs2_select_blocks_from_scores",
+            "hs2_paged_workspace_bytes", "hs2_paged_attn", "hs2_paged_attn_fp8", "hs2_paged_window_attn",
+            "hs2_paged_window_attn_fp8", "hs2_paged_append", "hs2_paged_append_fp8", "hs2_pages_extend",
+            "hs2_pages_reorder", "hs2_pages_compact", "hs2_pages_copy",
             "hs2_sparse_attn_noalloc", "hs2_stream_read_probe", "hs2_status_string", "hs2_last_error", "hs2_timing_enable",
             "hs2_timing_reset", "hs2_timing_read"]
 
@@ -38,6 +42,13 @@ class hs2_dims(ctypes.Structure):
                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("max_len", ctypes.c_int32),
                 ("kv_stride_b", ctypes.c_int64), ("kv_stride_h", ctypes.c_int64), ("kv_stride_t", ctypes.c_int64),
                 ("scale", ctypes.c_float)]
+
+
+class hs2_paged_dims(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_queries", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("kv_stride_p", ctypes.c_int64),
+                ("kv_stride_h", ctypes.c_int64), ("kv_stride_t", ctypes.c_int64), ("scale", ctypes.c_float)]
 
 
 class HS2Error(RuntimeError):
@@ -81,6 +92,21 @@ def load() -> ctypes.CDLL:
     lib.hs2_sparse_attn_noalloc.restype = I32
     lib.hs2_stream_read_probe.argtypes = [P, SZ, I32, P, P]
     lib.hs2_stream_read_probe.restype = I32
+    PD, I64 = ctypes.POINTER(hs2_paged_dims), ctypes.c_int64
+    lib.hs2_paged_workspace_bytes.argtypes = [PD]
+    lib.hs2_paged_workspace_bytes.restype = SZ
+    for name, args in (("hs2_paged_attn", [PD] + [P] * 9 + [SZ, P]),
+                       ("hs2_paged_attn_fp8", [PD] + [P] * 11 + [SZ, P]),
+                       ("hs2_paged_window_attn", [PD] + [P] * 5 + [I32, I32] + [P] * 4 + [SZ, P]),
+                       ("hs2_paged_window_attn_fp8", [PD] + [P] * 7 + [I32, I32] + [P] * 4 + [SZ, P]),
+                       ("hs2_paged_append", [PD, P, P, I64, I64, I64, I32] + [P] * 6),
+                       ("hs2_paged_append_fp8", [PD, P, P, I64, I64, I64, I32] + [P] * 8),
+                       ("hs2_pages_extend", [PD] + [P] * 7 + [SZ, P]),
+                       ("hs2_pages_reorder", [PD] + [P] * 8 + [I32, P, P, SZ, P]),
+                       ("hs2_pages_compact", [PD] + [P] * 5 + [I32, P, P, SZ, P]),
+                       ("hs2_pages_copy", [PD, P, P, I32, I32, P, P, P])):
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = I32
     lib.hs2_status_string.argtypes = [I32]
     lib.hs2_status_string.restype = ctypes.c_char_p
     lib.hs2_last_error.argtypes = []
@@ -333,6 +359,192 @@ def hs2_select_from_scores(dims, scores, len, k, window, idx, workspace, stream=
                                          _stream(stream)))
 
 
+# ------------------------------------------------------------------ paged cache
+def make_paged_dims(batch, n_queries, n_q_heads, n_kv_heads, head_dim, page, n_pages, max_pages, kv_strides=None,
+                    scale=0.0) -> hs2_paged_dims:
+    """Dims of a contiguous [n_pages, Hkv, page, D] pool unless strides (page, KV head, token) are given."""
+    if kv_strides is None:
+        kv_strides = (n_kv_heads * page * head_dim, page * head_dim, head_dim)
+    return hs2_paged_dims(batch, n_queries, n_q_heads, n_kv_heads, head_dim, page, n_pages, max_pages, *kv_strides,
+                          scale)
+
+
+def hs2_paged_workspace_bytes(dims: hs2_paged_dims) -> int:
+    return int(load().hs2_paged_workspace_bytes(ctypes.byref(dims)))
+
+
+_I32 = (torch.int32,)
+_F32 = (torch.float32,)
+
+
+def _current(device):
+    """The kernels run on the current device: its tensors only."""
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on the current HIP device expected, got {device}")
+
+
+def _check_pool(dims, K, V, device, fp8):
+    dtypes, what = (_FP8, "E4M3 (uint8)") if fp8 else (_BF16, "bf16")
+    last = ((dims.n_pages - 1) * dims.kv_stride_p + (dims.n_kv_heads - 1) * dims.kv_stride_h
+            + (dims.page - 1) * dims.kv_stride_t + dims.head_dim)
+    for name, t in (("K", K), ("V", V)):
+        if t.dtype not in dtypes or t.device != device:
+            raise ValueError(f"{name}: {what} tensor on {device} expected")
+        avail = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+        if last > avail:
+            raise ValueError(f"{name}: strides address {last} elements, storage holds {avail}")
+
+
+def _workspace(workspace, device):
+    if workspace is None or workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: a contiguous tensor on {device} is required")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _paged_attn(dims, q, K, V, scales, table, len, span, sink, gate, out, workspace, stream):
+    dev = q.device
+    _current(dev)
+    B, C, Hq, D = dims.batch, dims.n_queries, dims.n_q_heads, dims.head_dim
+    shape = (B, C, Hq, D)
+    _expect(q, "q", shape, _BF16, dev)
+    _check_pool(dims, K, V, dev, scales is not None)
+    if scales is not None:
+        _check_scales(dims, scales[0], scales[1], dev)
+    _expect(table, "table", (B, dims.max_pages), _I32, dev)
+    _expect(len, "len", (B,), _I32, dev)
+    if sink is not None:
+        _expect(sink, "sink", (Hq,), _F32, dev)
+    if gate is not None:
+        _expect(gate, "gate", shape, _BF16, dev)
+    _expect(out, "out", shape, _BF16, dev)
+    ws, ws_bytes = _workspace(workspace, dev)
+    name = "hs2_paged_attn" if span is None else "hs2_paged_window_attn"
+    call = getattr(load(), name if scales is None else name + "_fp8")
+    args = [] if scales is None else [_ptr(scales[0]), _ptr(scales[1])]
+    span = () if span is None else (int(span[0]), int(span[1]))
+    _check(call(ctypes.byref(dims), _ptr(q), _ptr(K), _ptr(V), *args, _ptr(table), _ptr(len), *span, _ptr(sink),
+                _ptr(gate), _ptr(out), ws, ws_bytes, _stream(stream)))
+
+
+def hs2_paged_attn(dims, q, K, V, table, len, sink, gate, out, workspace, stream=None):
+    """Attention of the new tokens over every token of their sequences in a paged cache; per-head sink logits [Hq]
+    float32 and output gate logits [B, C, Hq, D] bf16 may be None."""
+    _paged_attn(dims, q, K, V, None, table, len, None, sink, gate, out, workspace, stream)
+
+
+def hs2_paged_attn_fp8(dims, q, K8, V8, k_scale, v_scale, table, len, sink, gate, out, workspace, stream=None):
+    """hs2_paged_attn over an E4M3 pool (uint8 K8/V8, fp32 scales [Hkv])."""
+    _paged_attn(dims, q, K8, V8, (k_scale, v_scale), table, len, None, sink, gate, out, workspace, stream)
+
+
+def hs2_paged_window_attn(dims, q, K, V, table, len, window, first, sink, gate, out, workspace, stream=None):
+    """hs2_paged_attn over the `window` most recent tokens and the `first` first ones."""
+    _paged_attn(dims, q, K, V, None, table, len, (window, first), sink, gate, out, workspace, stream)
+
+
+def hs2_paged_window_attn_fp8(dims, q, K8, V8, k_scale, v_scale, table, len, window, first, sink, gate, out, workspace,
+                              stream=None):
+    """hs2_paged_window_attn over an E4M3 pool."""
+    _paged_attn(dims, q, K8, V8, (k_scale, v_scale), table, len, (window, first), sink, gate, out, workspace, stream)
+
+
+def _paged_append(dims, k_new, v_new, n_new, scales, table, len, K, V, stream):
+    dev = k_new.device
+    _current(dev)
+    B, Hkv, D = dims.batch, dims.n_kv_heads, dims.head_dim
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        if t.dim() != 4 or (t.shape[0], t.shape[2], t.shape[3]) != (B, Hkv, D) or t.shape[1] < 1:
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected ({B}, tokens, {Hkv}, {D})")
+        if t.dtype not in _BF16 or t.device != dev or t.stride(3) != 1:
+            raise ValueError(f"{name}: bf16 rows of contiguous elements on {dev} expected")
+    if k_new.shape != v_new.shape or k_new.stride() != v_new.stride():
+        raise ValueError("k_new and v_new: one shape and one set of strides expected")
+    if n_new is not None:
+        _expect(n_new, "n_new", (B,), _I32, dev)
+    _check_pool(dims, K, V, dev, scales is not None)
+    if scales is not None:
+        _check_scales(dims, scales[0], scales[1], dev)
+    _expect(table, "table", (B, dims.max_pages), _I32, dev)
+    _expect(len, "len", (B,), _I32, dev)
+    sb, st, sh, _ = k_new.stride()
+    call = load().hs2_paged_append if scales is None else load().hs2_paged_append_fp8
+    args = [] if scales is None else [_ptr(scales[0]), _ptr(scales[1])]
+    _check(call(ctypes.byref(dims), _ptr(k_new), _ptr(v_new), sb, st, sh, k_new.shape[1], _ptr(n_new), *args,
+                _ptr(table), _ptr(len), _ptr(K), _ptr(V), _stream(stream)))
+
+
+def hs2_paged_append(dims, k_new, v_new, n_new, table, len, K, V, stream=None):
+    """Rows k_new, v_new [B, T, Hkv, D] bf16 (any strides between rows) to the last T tokens of each sequence, or the
+    first n_new[b] rows to the last n_new[b] tokens (n_new [B] int32, or None)."""
+    _paged_append(dims, k_new, v_new, n_new, None, table, len, K, V, stream)
+
+
+def hs2_paged_append_fp8(dims, k_new, v_new, n_new, k_scale, v_scale, table, len, K8, V8, stream=None):
+    """hs2_paged_append into an E4M3 pool: the values nearest to row / scale."""
+    _paged_append(dims, k_new, v_new, n_new, (k_scale, v_scale), table, len, K8, V8, stream)
+
+
+def _pages(dims, table, refs, table_out, refs_out, counts, workspace):
+    dev = table.device
+    _current(dev)
+    shape = (dims.batch, dims.max_pages)
+    _expect(table, "table", shape, _I32, dev)
+    _expect(table_out, "table_out", shape, _I32, dev)
+    _expect(refs, "refs", (dims.n_pages,), _I32, dev)
+    _expect(refs_out, "refs_out", (dims.n_pages,), _I32, dev)
+    _expect(counts, "counts", (2,), _I32, dev)
+    return dev, *_workspace(workspace, dev)
+
+
+def _expect_moves(moves, least, device):
+    if moves.dim() != 2 or moves.shape[0] < least:
+        raise ValueError(f"moves: shape {tuple(moves.shape)}, at least ({least}, 3) expected")
+    _expect(moves, "moves", (moves.shape[0], 3), _I32, device)
+
+
+def hs2_pages_extend(dims, table, len, refs, table_out, refs_out, counts, workspace, stream=None):
+    """Free pages for every row that holds fewer than len[b] tokens need; table_out and refs_out may be the inputs."""
+    dev, ws, ws_bytes = _pages(dims, table, refs, table_out, refs_out, counts, workspace)
+    _expect(len, "len", (dims.batch,), _I32, dev)
+    _check(load().hs2_pages_extend(ctypes.byref(dims), _ptr(table), _ptr(len), _ptr(refs), _ptr(table_out),
+                                   _ptr(refs_out), _ptr(counts), ws, ws_bytes, _stream(stream)))
+
+
+def hs2_pages_reorder(dims, parent, table, len, refs, table_out, len_out, refs_out, moves, counts, workspace,
+                      stream=None):
+    """Every row takes over its parent row's tokens (a fork, a permutation; a parent outside [0, B) frees the row);
+    hs2_pages_copy has to copy the moves in every layer's pool."""
+    dev, ws, ws_bytes = _pages(dims, table, refs, table_out, refs_out, counts, workspace)
+    for name, t in (("parent", parent), ("len", len), ("len_out", len_out)):
+        _expect(t, name, (dims.batch,), _I32, dev)
+    _expect_moves(moves, dims.batch, dev)
+    _check(load().hs2_pages_reorder(ctypes.byref(dims), _ptr(parent), _ptr(table), _ptr(len), _ptr(refs),
+                                    _ptr(table_out), _ptr(len_out), _ptr(refs_out), _ptr(moves), moves.shape[0],
+                                    _ptr(counts), ws, ws_bytes, _stream(stream)))
+
+
+def hs2_pages_compact(dims, table, refs, table_out, refs_out, moves, counts, workspace, stream=None):
+    """Packs the used pages to the front of the pool; hs2_pages_copy has to copy the moves in every layer's pool."""
+    dev, ws, ws_bytes = _pages(dims, table, refs, table_out, refs_out, counts, workspace)
+    _expect_moves(moves, max(1, dims.n_pages // 2), dev)
+    _check(load().hs2_pages_compact(ctypes.byref(dims), _ptr(table), _ptr(refs), _ptr(table_out), _ptr(refs_out),
+                                    _ptr(moves), moves.shape[0], _ptr(counts), ws, ws_bytes, _stream(stream)))
+
+
+def hs2_pages_copy(dims, moves, n_moves, K, V, stream=None):
+    """Copies the first n_moves[0] moves (int32 on the device, as the calls above leave it) in one layer's pool."""
+    dev = K.device
+    _current(dev)
+    _expect_moves(moves, 0, dev)
+    if n_moves.dtype != torch.int32 or n_moves.device != dev or n_moves.numel() < 1:
+        raise ValueError(f"n_moves: int32 on {dev} expected")
+    fp8 = K.dtype in _FP8
+    _check_pool(dims, K, V, dev, fp8)
+    if moves.shape[0]:
+        _check(load().hs2_pages_copy(ctypes.byref(dims), _ptr(moves), _ptr(n_moves), moves.shape[0], 1 if fp8 else 2,
+                                     _ptr(K), _ptr(V), _stream(stream)))
+
+
 STREAM_PROBE_SINK_WORDS = 4096
 
 
@@ -432,3 +644,92 @@ class HybridBlock:
         else:
             hs2_sparse_attn_ex(d, q, K, V, lens, idx, idx.shape[-1], sink, gate, out, self.workspace, stream)
         return out
+
+
+class PagedCache:
+    """Convenience wrapper: one layer's paged cache of `batch` sequences, with its table, counts and workspace.
+
+    ``extend(n)`` makes room for n more tokens of each sequence, ``append(k, v)`` writes them, ``attend(q)`` attends
+    over every token (``window=``, ``first=``: over the recent and the first ones); ``reorder(parent)`` forks, permutes
+    and frees sequences, ``compact()`` packs the pool.  With ``kv_scales=(k_scale, v_scale)`` the pool is E4M3.  No
+    call waits for the device; the tensors ``K``, ``V``, ``table``, ``len`` and ``refs`` keep their addresses, so calls
+    can be captured in a graph.  ``counts`` holds what the last of extend, reorder and compact reported: counts[1] of
+    an extend or a reorder is the number of pages that the pool did not have.
+    """
+
+    def __init__(self, batch, n_q_heads, n_kv_heads, head_dim, page, n_pages, max_pages, device="cuda", kv_scales=None,
+                 scale=0.0):
+        device = torch.device(device)
+        if device.index is None:
+            device = torch.device(device.type, torch.cuda.current_device())
+        # K and V of a token side by side: one record of 2 D elements
+        pool = torch.empty((n_pages, n_kv_heads, page, 2 * head_dim), device=device,
+                           dtype=torch.bfloat16 if kv_scales is None else torch.uint8)
+        self.K, self.V, self.kv_scales = pool[..., :head_dim], pool[..., head_dim:], kv_scales
+        self._shape = (n_q_heads, n_kv_heads, head_dim, page, n_pages, max_pages, tuple(self.K.stride()[:3]), scale)
+        self._dims, self.batch = {}, batch
+
+        def ints(*shape, fill=0):
+            return torch.full(shape, fill, dtype=torch.int32, device=device)
+        self.table, self.len, self.refs = ints(batch, max_pages, fill=-1), ints(batch), ints(n_pages)
+        self._table, self._len = torch.empty_like(self.table), torch.empty_like(self.len)
+        self.moves, self.counts = ints(max(batch, n_pages // 2, 1), 3), ints(2)
+        if hs2_paged_workspace_bytes(self.dims(1)) == 0:
+            raise HS2Error(HS2_ERR_SHAPE, hs2_last_error())
+        need = max(hs2_paged_workspace_bytes(self.dims(c)) for c in range(1, 17))  # 0 past the largest chunk
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
+
+    def dims(self, n_queries):
+        d = self._dims.get(n_queries)
+        if d is None:
+            d = self._dims[n_queries] = make_paged_dims(self.batch, n_queries, *self._shape)
+        return d
+
+    def extend(self, n, stream=None):
+        """n: tokens (an int, or int32 [batch]) that every sequence grows by."""
+        with self._on(stream):
+            self.len.add_(n)
+        hs2_pages_extend(self.dims(1), self.table, self.len, self.refs, self.table, self.refs, self.counts,
+                         self.workspace, stream)
+
+    def append(self, k, v, n_new=None, stream=None):
+        """k, v [batch, T, Hkv, D] bf16: the last T tokens of each sequence (the last n_new[b], first rows first)."""
+        if self.kv_scales is None:
+            hs2_paged_append(self.dims(1), k, v, n_new, self.table, self.len, self.K, self.V, stream)
+        else:
+            hs2_paged_append_fp8(self.dims(1), k, v, n_new, *self.kv_scales, self.table, self.len, self.K, self.V,
+                                 stream)
+
+    def attend(self, q, window=None, first=0, sink=None, gate=None, out=None, stream=None):
+        """q [batch, C, Hq, D] bf16, the queries of the last C tokens of each sequence; returns out."""
+        d = self.dims(q.shape[1])
+        if out is None:
+            with self._on(stream):
+                out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        _paged_attn(d, q, self.K, self.V, self.kv_scales, self.table, self.len,
+                    None if window is None else (window, first), sink, gate, out, self.workspace, stream)
+        return out
+
+    def reorder(self, parent, stream=None):
+        """Row b becomes a copy of row parent[b] (int32 [batch]; outside [0, batch): freed)."""
+        d = self.dims(1)
+        hs2_pages_reorder(d, parent, self.table, self.len, self.refs, self._table, self._len, self.refs, self.moves,
+                          self.counts, self.workspace, stream)
+        hs2_pages_copy(d, self.moves[:self.batch], self.counts, self.K, self.V, stream)
+        with self._on(stream):
+            self.table.copy_(self._table)
+            self.len.copy_(self._len)
+
+    def compact(self, stream=None):
+        d = self.dims(1)
+        hs2_pages_compact(d, self.table, self.refs, self.table, self.refs, self.moves, self.counts, self.workspace,
+                          stream)
+        hs2_pages_copy(d, self.moves, self.counts, self.K, self.V, stream)
+
+    @staticmethod
+    def _on(stream):
+        if stream is None:
+            return contextlib.nullcontext()
+        if not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream))
+        return torch.cuda.stream(stream)
