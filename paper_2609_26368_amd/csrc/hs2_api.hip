@@ -435,6 +435,7 @@ hs2_status ensure_device_init(const DeviceInfo** info) {
   std::lock_guard<std::mutex> lk(g_init_mu);
   if (!g_dev_done[dev]) {
     hipError_t e = set_pool_smem_limits();
+    if (e == hipSuccess) e = set_paged_smem_limits();
     if (e != hipSuccess) return fail(HS2_ERR_HIP, "hipFuncSetAttribute: %s", hipGetErrorString(e));
     DeviceInfo di;
     if ((e = hipDeviceGetAttribute(&di.cus, hipDeviceAttributeMultiprocessorCount, dev)) != hipSuccess)
@@ -971,6 +972,8 @@ hs2_status hs2_stream_read_probe(const void* src, size_t bytes, int32_t mode, ui
 namespace {
 
 constexpr int kMaxPages = 1 << 24;  // of a pool: their chunks' prefix sums sit in LDS
+// paged attention of at most so many 16-token blocks: one workgroup finishes a KV head
+constexpr int kPagedSingleBlocks = 64;
 
 // kv8: E4M3 strides
 hs2_status check_paged(const hs2_paged_dims* d, bool kv8) {
@@ -1027,6 +1030,41 @@ PagesPlan pages_plan(const hs2_paged_dims* d) {
   return p;
 }
 
+// Splits and workspace of the paged attention.
+struct PagedPlan {
+  int RT, rows;
+  PagedSplit sp;
+  size_t off_part_o, off_part_ml, off_units, bytes;
+};
+PagedPlan paged_plan(const hs2_paged_dims* d, bool kv8, int32_t window, int32_t first, const DeviceInfo* di) {
+  PagedPlan p;
+  const int G = d->n_q_heads / d->n_kv_heads;
+  p.RT = next_pow2((int)cdiv(d->n_queries * next_pow2(G), 16));
+  const PagedAttnShape sh = paged_attn_shape(p.RT, kv8, d->head_dim);
+  p.rows = sh.rows;
+  const int64_t units = (int64_t)d->batch * d->n_kv_heads;
+  const int64_t cus = di ? di->cus : 256, round = cus * sh.wgs;
+  // the most blocks that a chunk can see
+  int64_t cap = cdiv((int64_t)d->page * d->max_pages, 16);
+  if (window > 0) cap = std::min(cap, cdiv(first, 16) + cdiv((int64_t)window + d->n_queries - 1, 16) + 1);
+  p.sp.cap_blocks = (int)cap;
+  p.sp.align = sh.align;
+  p.sp.single = cap <= kPagedSingleBlocks;
+  p.sp.fixed = p.sp.single ? (int)round_up(cap, sh.align) : 0;
+  p.sp.min_blocks = (int)round_up(16, sh.align);
+  p.sp.few_items = (int)std::min(cus, round);
+  // up to four rounds where the KV heads would not be cut evenly in one
+  const int64_t balance = std::min<int64_t>(4, std::max<int64_t>(1, cdiv(4 * units, round)));
+  p.sp.n_items = (int)std::min(std::max(round * balance, units + round / 4), units * cdiv(cap, sh.align));
+  size_t cur = 0;
+  const int64_t rows = p.sp.single ? 0 : (int64_t)p.sp.n_items * p.rows;
+  p.off_part_o = carve(cur, sizeof(float) * rows * d->head_dim);
+  p.off_part_ml = carve(cur, sizeof(float) * rows * 2);
+  p.off_units = carve(cur, sizeof(int32_t) * units * 2);
+  p.bytes = (size_t)round_up((int64_t)cur, kAlign);
+  return p;
+}
+
 // window 0: every token
 hs2_status paged_attn_impl(const hs2_paged_dims* d, const uint16_t* q, const void* K, const void* V, bool kv8,
                            const float* k_scale, const float* v_scale, const int32_t* table, const int32_t* len,
@@ -1042,12 +1080,19 @@ hs2_status paged_attn_impl(const hs2_paged_dims* d, const uint16_t* q, const voi
       (kv8 && (!aligned(k_scale, 4) || !aligned(v_scale, 4))))
     return fail(HS2_ERR_ALIGN,
                 "q/K/V/out need 16-byte, workspace 256-byte, gate 8-byte, table/len/sink/scales 4-byte alignment");
-  const size_t need = hs2_paged_workspace_bytes(d);
-  if (workspace_bytes < need)
-    return fail(HS2_ERR_WORKSPACE, "workspace %zu bytes < %zu required", workspace_bytes, need);
-  if ((st = ensure_device_init(nullptr)) != HS2_OK) return st;
+  const DeviceInfo* di = try_device_info();
+  const PagedPlan plan = paged_plan(d, kv8, window, first, di);
+  if (workspace_bytes < plan.bytes)
+    return fail(HS2_ERR_WORKSPACE, "workspace %zu bytes < %zu required", workspace_bytes, plan.bytes);
+  if ((st = ensure_device_init(&di)) != HS2_OK) return st;
   PagedAttnArgs a{};
   a.p = paged_pool(d, K, V, table, len, kv8 ? 1 : 2);
+  a.sp = plan.sp;
+  char* ws = (char*)workspace;
+  a.part_o = (float*)(ws + plan.off_part_o);
+  a.part_ml = (float*)(ws + plan.off_part_ml);
+  a.unit_items = (int32_t*)(ws + plan.off_units);
+  a.part_rows = plan.rows;
   a.q = q;
   a.out = out;
   const double scale = d->scale > 0.f ? (double)d->scale : 1.0 / std::sqrt((double)d->head_dim);
@@ -1062,7 +1107,9 @@ hs2_status paged_attn_impl(const hs2_paged_dims* d, const uint16_t* q, const voi
   a.v_scale = v_scale;
   a.sink = sink;
   a.gate = gate;
-  HS2_TRY_LAUNCH(KK_PAGED_ATTN, (hipStream_t)stream, launch_paged_attn(a, (hipStream_t)stream));
+  hipStream_t s = (hipStream_t)stream;
+  HS2_TRY_LAUNCH(KK_PAGED_ATTN, s, launch_paged_attn(a, plan.RT, s));
+  if (!a.sp.single) HS2_TRY_LAUNCH(KK_PAGED_MERGE, s, launch_paged_merge(a, s));
   return HS2_OK;
 }
 
@@ -1142,7 +1189,11 @@ extern "C" {
 
 size_t hs2_paged_workspace_bytes(const hs2_paged_dims* d) {
   if (check_paged(d, false) != HS2_OK) return 0;
-  return pages_plan(d).bytes;
+  const DeviceInfo* di = try_device_info();
+  size_t bytes = pages_plan(d).bytes;
+  for (int kv8 = 0; kv8 < 2; ++kv8)  // either pool format; a window's blocks are among all
+    bytes = std::max(bytes, paged_plan(d, kv8 == 1, 0, 0, di).bytes);
+  return bytes;
 }
 
 hs2_status hs2_paged_attn(const hs2_paged_dims* d, const uint16_t* q, const uint16_t* K, const uint16_t* V,

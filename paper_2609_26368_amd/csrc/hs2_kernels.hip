@@ -69,34 +69,6 @@ __device__ inline void load_q_tile(uint4 (&q)[NKK], const uint16_t* __restrict__
 // load, so they are kept short: 32-bit sums and scans through DPP lane moves
 // (no LDS permutes), and a bracket from float arithmetic (64-bit divisions
 // and shuffled 64-bit sums here took 3-5 us of each launch).
-// A lane move: lane l receives v of the lane that CTRL names, 0 where there
-// is none (or where ROWS masks its row of 16 out).
-template <int CTRL, int ROWS>
-__device__ inline int dpp_move(int v) {
-  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, true);
-}
-// inclusive prefix sums over the wave's lanes (all 64 active)
-__device__ inline int wave_scan(int v) {
-  v += dpp_move<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8: prefix within each row of 16
-  v += dpp_move<0x112, 0xF>(v);
-  v += dpp_move<0x114, 0xF>(v);
-  v += dpp_move<0x118, 0xF>(v);
-  v += dpp_move<0x142, 0xA>(v);  // row_bcast 15: rows 1 and 3 add the row before
-  v += dpp_move<0x143, 0xC>(v);  // row_bcast 31: rows 2 and 3 add the first half
-  return v;
-}
-__device__ inline int wave_sum(int v) { return __builtin_amdgcn_readlane(wave_scan(v), 63); }
-__device__ inline float wave_sum(float v) {
-  auto add = [](float a, int b) { return a + __int_as_float(b); };
-  v = add(v, dpp_move<0x111, 0xF>(__float_as_int(v)));
-  v = add(v, dpp_move<0x112, 0xF>(__float_as_int(v)));
-  v = add(v, dpp_move<0x114, 0xF>(__float_as_int(v)));
-  v = add(v, dpp_move<0x118, 0xF>(__float_as_int(v)));
-  v = add(v, dpp_move<0x142, 0xA>(__float_as_int(v)));
-  v = add(v, dpp_move<0x143, 0xC>(__float_as_int(v)));
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
-}
-
 __device__ inline int splits_of(int L, int S) { return (int)(((uint32_t)L + (uint32_t)S - 1u) / (uint32_t)S); }
 
 // The clamped lengths of the sequences b = lane, lane + 64, ...: the first

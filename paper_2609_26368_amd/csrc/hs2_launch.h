@@ -186,8 +186,21 @@ struct PagedPool {
   int B, Hkv, hd, page, page_shift, n_pages, max_pages;
 };
 
+// Splits of the paged attention, in blocks of 16 tokens: fixed > 0 fixes their
+// length (single: one a KV head, the grid's workgroups are the KV heads); else
+// every workgroup derives it from len[] (paged_split_blocks).
+struct PagedSplit {
+  int fixed, align, min_blocks, n_items, few_items, cap_blocks;
+  bool single;
+};
+
 struct PagedAttnArgs {
   PagedPool p;
+  PagedSplit sp;
+  float* part_o;           // [n_items][part_rows][hd]: splits' unnormalised outputs
+  float* part_ml;          // [n_items][part_rows][2]: (m, l)
+  int32_t* unit_items;     // [B * Hkv][2]: first item and number of items of each KV head
+  int part_rows;
   const uint16_t* q;
   uint16_t* out;           // [B, C, Hq, hd]
   float c2;                // softmax scale * log2(e)
@@ -198,7 +211,13 @@ struct PagedAttnArgs {
   const float* sink;       // [Hq] or null
   const uint16_t* gate;    // [B, C, Hq, hd] or null
 };
-hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
+struct PagedAttnShape {
+  int rows, align, wgs;  // partial rows, blocks that splits are multiples of, workgroups per compute unit
+};
+PagedAttnShape paged_attn_shape(int RT, bool kv8, int hd);
+hipError_t set_paged_smem_limits();
+hipError_t launch_paged_attn(const PagedAttnArgs& a, int RT, hipStream_t s);
+hipError_t launch_paged_merge(const PagedAttnArgs& a, hipStream_t s);
 
 struct PagedAppendArgs {
   PagedPool p;

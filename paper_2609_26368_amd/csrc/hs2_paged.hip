@@ -1,6 +1,7 @@
 // HIP kernels of the paged KV cache (gfx950).
 //
-//   k_paged_attn     attention of the new tokens over a sequence's pages
+//   k_paged_attn     attention of the new tokens over a sequence's pages, split over
+//                    its length; k_paged_merge joins the splits
 //   k_paged_append   new K and V rows to their slots (bf16, or quantised to E4M3)
 //   k_pages_scan     lists the free pages of each chunk of the pool (compaction:
 //                    counts the used ones) and what each table row wants
@@ -23,83 +24,583 @@ __device__ inline int paged_len(const PagedPool& p, int b) {
 __device__ inline bool is_page(int id, int n_pages) { return (uint32_t)id < (uint32_t)n_pages; }
 
 // ============================================================================ attention
-// grid (Hq, C, B), 4 waves: wave w takes every fourth token that the query
-// sees, a lane HDIM / 64 of its head dims; the waves meet in LDS.
-template <bool KV8, int HDIM>
-__global__ __launch_bounds__(NTP) void k_paged_attn(PagedAttnArgs a) {
-  constexpr int EPL = HDIM / 64, NW = NTP / 64;
-  __shared__ float s_m[NW], s_l[NW], s_o[NW][HDIM];
-  const int h = blockIdx.x, c = blockIdx.y, b = blockIdx.z, g = h / a.G;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int pos = paged_len(a.p, b) - a.C + c;
-  const int64_t orow = ((int64_t)b * a.C + c) * a.Hq + h;
-  // the tokens seen: [0, nf), then [w0, pos]
-  const int w0 = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
-  const int nf = min(a.first, w0);
-  const int n = pos < 0 ? 0 : nf + pos + 1 - w0;
-  float q[EPL], o[EPL];
-#pragma unroll
-  for (int j = 0; j < EPL; ++j) {
-    q[j] = bf16_bits_to_f32(a.q[orow * HDIM + lane * EPL + j]) * a.c2 * (KV8 ? a.k_scale[g] : 1.f);
-    o[j] = 0.f;
+// Softmax attention of a chunk's queries over the pages of their sequence,
+// one pass over K and V with a running maximum and sum per query row:
+//   s_t = c2 <q, k_t>,  m' = max(m, s_t),  l' = l 2^(m - m') + 2^(s_t - m'),
+//   o' = o 2^(m - m') + 2^(s_t - m') v_t,  out = o / l   (c2 = scale log2 e).
+// Bound by reading K and V once: 4 G C operations a byte of a bf16 cache, far
+// below the matrix units' rate.
+//
+// Tokens are taken in blocks of 16, which never straddle a page.  The blocks
+// that some query of the chunk sees are numbered through: nf blocks of first
+// tokens, then those from the start of the earliest query's window on.  A
+// sequence's blocks are cut into splits of S (PagedSplit); a workgroup takes
+// one split of one KV head.  Its TGW token groups take every TGW-th tile of
+// TW tokens through an LDS ring of their own, and the NWV waves of a group
+// share its tiles, RPW row tiles of 16 query rows each.  A group of one wave
+// needs no barrier.  The groups meet in LDS; a KV head of one split is
+// finished there, of more it leaves partial rows for k_paged_merge.
+
+// The visible blocks of a sequence with Lv tokens.
+struct PagedSpan {
+  int nf, w0, n;  // blocks of first tokens, first block of the window, all of them
+};
+__device__ inline PagedSpan paged_span(const PagedAttnArgs& a, int Lv) {
+  PagedSpan s;
+  const int pos0 = max(0, Lv - a.C);  // the earliest query that sees anything
+  s.w0 = a.window > 0 ? max(0, pos0 - a.window + 1) / 16 : 0;
+  s.nf = min((a.first + 15) / 16, s.w0);
+  s.n = s.nf + (Lv + 15) / 16 - s.w0;
+  return s;
+}
+__device__ inline int token_block(const PagedSpan& s, int i) { return i < s.nf ? i : i - s.nf + s.w0; }
+
+// Sums over the wave of a value per sequence; f(blocks) of sequences lane, lane + 64, ...
+template <class F>
+__device__ inline int wave_sum_sequences(const PagedAttnArgs& a, int n0, F&& f) {
+  const int lane = threadIdx.x & 63;
+  int s = lane < a.p.B ? f(n0) : 0;
+  for (int b = lane + 64; b < a.p.B; b += 64) s += f(paged_span(a, paged_len(a.p, b)).n);
+  return wave_sum(s);
+}
+__device__ inline int splits_at(int n, int S) { return max(1, (n + S - 1) / S); }
+
+// Blocks per split: the shortest multiple of align, at least min_blocks, whose
+// (sequence, KV head, split) items number at most n_items (few tokens: at
+// most few_items, with splits down to align).  items(S) lies between total / S and total / S +
+// units, which brackets the search.
+__device__ inline int paged_split_blocks(const PagedAttnArgs& a, int n0) {
+  const PagedSplit& sp = a.sp;
+  if (sp.fixed) return sp.fixed;
+  const int units = a.p.B * a.p.Hkv;
+  float tot = 0.f;
+  {
+    const int lane = threadIdx.x & 63;
+    if (lane < a.p.B) tot = (float)n0;
+    for (int b = lane + 64; b < a.p.B; b += 64) tot += (float)paged_span(a, paged_len(a.p, b)).n;
+    tot = wave_sum(tot) * (float)a.p.Hkv;
   }
-  auto load = [&](const unsigned char* row, float (&x)[EPL]) {
-    if constexpr (KV8) {
+  const bool few = sp.few_items > units && tot <= (float)sp.min_blocks * (float)sp.few_items;
+  const int n_items = few ? sp.few_items : sp.n_items;
+  const float n = (float)n_items, al = (float)sp.align;
+  int lo = max(few ? 1 : sp.min_blocks / sp.align, (int)(tot * (0.9999f / (n * al))));
+  int hi = (sp.cap_blocks + sp.align - 1) / sp.align;
+  if (n_items > units) hi = min(hi, (int)fminf(tot * (1.0001f / ((n - (float)units) * al)), 1e9f) + 1);
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(max(hi, lo));
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2, S = mid * sp.align;
+    if (wave_sum_sequences(a, n0, [&](int k) { return splits_at(k, S); }) * a.p.Hkv <= n_items)
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  return hi * sp.align;
+}
+
+// The (sequence, KV head, split) of a workgroup, how many splits that KV head
+// has; false past the last item.
+struct PagedItem {
+  int b, g, split, n_splits;
+};
+__device__ inline bool paged_locate(const PagedAttnArgs& a, int n0, int S, int item, PagedItem& it) {
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < a.p.B; b0 += 64) {
+    const int b = b0 + lane;
+    const int k = b < a.p.B ? splits_at(b0 == 0 ? n0 : paged_span(a, paged_len(a.p, b)).n, S) : 0;
+    const int incl = wave_scan(k * a.p.Hkv);
+    const unsigned long long hit = __ballot(incl > item);
+    if (hit) {
+      const int l = __ffsll((long long)hit) - 1;
+      it.n_splits = __builtin_amdgcn_readlane(k, l);
+      const int r = item - (__builtin_amdgcn_readlane(incl, l) - it.n_splits * a.p.Hkv);
+      it.b = b0 + l;
+      it.g = r / it.n_splits;
+      it.split = r % it.n_splits;
+      return true;
+    }
+    item -= __builtin_amdgcn_readlane(incl, 63);
+  }
+  return false;
+}
+
+// Running softmax with BPW blocks of logits (log2 units, -inf: not seen);
+// returns the probabilities as A operands of P V.  They are rounded to bf16,
+// the cache's type (half a step, 2^-8), and the normaliser sums the rounded
+// values, so that the weights still sum to one.  m is raised only past
+// LAZY_MARGIN.
+template <int RPW, int BPW, int HDIM>
+__device__ inline void paged_softmax(WaveState<RPW, HDIM>& st, f32x4 (&S)[BPW][RPW], PFrags<BPW, RPW>& pf, int lane) {
 #pragma unroll
-      for (int j = 0; j < EPL; j += 2) {
-        const uint32_t v = e4m3x2_to_bf16x2(*(const uint16_t*)(row + lane * EPL + j));
-        x[j] = bf16_bits_to_f32(v & 0xFFFFu);
-        x[j + 1] = bf16_bits_to_f32(v >> 16);
+  for (int rr = 0; rr < RPW; ++rr) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int bi = 0; bi < BPW; ++bi)
+      mx = fmaxf(mx, fmaxf(fmaxf(S[bi][rr][0], S[bi][rr][1]), fmaxf(S[bi][rr][2], S[bi][rr][3])));
+    mx = max_xor32(max_xor16(mx));
+    if (__ballot(mx > st.m[rr] + LAZY_MARGIN)) {
+      const float mnew = fmaxf(st.m[rr], mx);
+      const float alpha = mnew == -INFINITY ? 1.f : fast_exp2(st.m[rr] - mnew);  // m = -inf -> 0
+      st.m[rr] = mnew;
+      st.l[rr] *= alpha;
+      float a4[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a4[i] = __shfl(alpha, 4 * (lane >> 4) + i);
+#pragma unroll
+      for (int nb = 0; nb < WaveState<RPW, HDIM>::NBC; ++nb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.o[rr][nb][i] *= a4[i];
+    }
+    const float msub = st.m[rr] == -INFINITY ? 0.f : st.m[rr];
+    float psum = 0.f;
+#pragma unroll
+    for (int bi = 0; bi < BPW; ++bi) {
+      const uint32_t lo = pack_bf16x2(fast_exp2(S[bi][rr][0] - msub), fast_exp2(S[bi][rr][1] - msub));
+      const uint32_t hi = pack_bf16x2(fast_exp2(S[bi][rr][2] - msub), fast_exp2(S[bi][rr][3] - msub));
+      psum += (__uint_as_float(lo << 16) + __uint_as_float(lo & 0xFFFF0000u)) +
+              (__uint_as_float(hi << 16) + __uint_as_float(hi & 0xFFFF0000u));
+      pf.set(bi, rr, lo, hi);
+    }
+    st.l[rr] += psum;
+  }
+}
+
+// Whether a staged tile of bytes holds an infinity or NaN (bf16: exponent of
+// ones, E4M3: 0x7F), looked at by the whole wave.
+template <bool KV8, int BYTES>
+__device__ inline bool any_not_finite(const unsigned char* tile, int lane) {
+  uint32_t bad = 0;
+#pragma unroll
+  for (int k = 0; k < BYTES / 1024; ++k) {
+    const uint4 v = *(const uint4*)(tile + 1024 * k + 16 * lane);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      bad |= KV8 ? ((w[j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u
+                 : ((w[j] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+  }
+  return __any(bad != 0);
+}
+
+// V operand(s) of blocks of a tile: blocks 2 i and 2 i + 1 (K32) or block i.
+template <bool KV8, bool K32, int HDIM, int RB>
+__device__ inline uint4 v_operand(const unsigned char* v, int i, int nb, int lane) {
+  if constexpr (K32 && KV8) {
+    return v_operand_e4m3_pair<RB>(v, i, nb, lane);
+  } else if constexpr (K32) {
+    const uint2 x = v_operand_tr_at<HDIM>(v, 2 * i, nb, lane), y = v_operand_tr_at<HDIM>(v, 2 * i + 1, nb, lane);
+    return make_uint4(x.x, x.y, y.x, y.y);
+  } else if constexpr (KV8) {
+    const uint2 x = v_operand_e4m3<RB>(v, i, nb, lane);
+    return make_uint4(x.x, x.y, 0, 0);
+  } else {
+    const uint2 x = v_operand_tr_at<HDIM>(v, i, nb, lane);
+    return make_uint4(x.x, x.y, 0, 0);
+  }
+}
+
+// O += P V of a tile in which some rows are hidden from some queries and some
+// V is not finite: a product with a probability of 0 would still carry a NaN
+// into the rows of the queries that do not see it.  One pass per query, with
+// the rows that it does not see taken as 0, kept in that query's rows only.
+// seen(t4, j, c): whether query c sees token t4 + j of the lane's four.
+template <int RPW, int NB, int HDIM, bool KV8, int RB, class Seen>
+__device__ inline void pv_per_query(WaveState<RPW, HDIM>& st, const PFrags<NB, RPW>& pf, const unsigned char* v, int C,
+                                    int Gp, int rt0, int lane, Seen&& seen) {
+  constexpr bool K32 = NB % 2 == 0;
+  for (int c = 0; c < C; ++c) {
+#pragma unroll
+    for (int i = 0; i < (K32 ? NB / 2 : NB); ++i) {
+      uint32_t keep[4];  // of the lane's tokens, two a word, in the operand's order
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int bi = K32 ? 2 * i + (j >> 1) : i, t = 2 * (j & 1);
+        keep[j] = (seen(bi, t, c) ? 0xFFFFu : 0u) | (seen(bi, t + 1, c) ? 0xFFFF0000u : 0u);
       }
-    } else {
 #pragma unroll
-      for (int j = 0; j < EPL; ++j) x[j] = bf16_bits_to_f32(((const uint16_t*)row)[lane * EPL + j]);
+      for (int nb = 0; nb < HDIM / 16; ++nb) {
+        uint4 x = v_operand<KV8, K32, HDIM, RB>(v, i, nb, lane);
+        x.x &= keep[0];
+        x.y &= keep[1];
+        x.z &= keep[2];
+        x.w &= keep[3];
+#pragma unroll
+        for (int rr = 0; rr < RPW; ++rr) {
+          f32x4 d = {0.f, 0.f, 0.f, 0.f};
+          if constexpr (K32)
+            d = mfma_k32(pf.w[i][rr], x, d);
+          else
+            d = mfma_k16(pf.h[i][rr], make_uint2(x.x, x.y), d);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if ((16 * (rt0 + rr) + 4 * (lane >> 4) + k) / Gp == c) st.o[rr][nb][k] += d[k];
+        }
+      }
+    }
+  }
+}
+
+// Shapes: LDS of a workgroup and what follows from the template's numbers.
+template <int RPW_, int NWV_, int TGW_, int TW_, int NS_, bool KV8, int HDIM>
+struct PagedShape {
+  static constexpr int RPW = RPW_, NWV = NWV_, TGW = TGW_, TW = TW_, NS = NS_;
+  static constexpr int RT = RPW * NWV, NW = NWV * TGW, ROWS = 16 * RT;
+  static constexpr int RB = KV8 ? HDIM : 2 * HDIM;       // bytes of a staged cache row
+  static constexpr int SB = 2 * TW * RB;                 // stage: K rows, then V rows
+  static constexpr int LPM = TW * RB / 1024 / NWV;       // 1 KB loads per matrix per stage per wave
+  static constexpr int GB = fa_ring_group_bytes(NWV, TW, NS, KV8, HDIM);
+  static constexpr int IDS = 128;                        // page ids per wave, two halves
+  // columns per exchange of the groups' outputs
+  static constexpr int CW = TGW * ROWS * (HDIM + 4) * 4 <= (TGW * GB > 70000 ? TGW * GB : 70000) ? HDIM : HDIM / 2;
+  static constexpr int EXCH = TGW * ROWS * (CW + 4) * 4;
+  static constexpr int RING = TGW * GB > EXCH ? TGW * GB : EXCH;
+  static constexpr int LDS = RING + NW * IDS * 4;
+  // workgroups per compute unit: each with its statistics and 1 KB to spare in 160 KB
+  static constexpr int WGS = 160 * 1024 / (LDS + TGW * ROWS * 8 + 1024);
+  static_assert(LPM >= 1 && TW * RB == 1024 * LPM * NWV, "whole 1 KB loads for every wave and stage");
+};
+
+// Weight of a part with maximum m against the common maximum M (0 where it
+// has seen nothing; a NaN of its sums stays one).
+__device__ inline float merge_weight(float m, float M) { return m == -INFINITY ? 0.f : fast_exp2(m - M); }
+
+// Four columns of a finished row: over Z, times the cache's scale and the
+// gate's sigmoid, rounded to bf16.
+__device__ inline void paged_store4(float4 o, float Z, float v_scale, const uint16_t* gate, uint16_t* out) {
+  const float inv = (Z > 0.f || Z != Z ? 1.f / Z : 0.f) * v_scale;
+  float x[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+  if (gate) {
+    const uint2 gb = *(const uint2*)gate;
+    const float gv[4] = {bf16_bits_to_f32(gb.x & 0xFFFFu), bf16_bits_to_f32(gb.x >> 16),
+                         bf16_bits_to_f32(gb.y & 0xFFFFu), bf16_bits_to_f32(gb.y >> 16)};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] *= 1.f / (1.f + fast_exp2(-gv[j] * 1.4426950408889634f));
+  }
+  *(uint2*)out = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+}
+
+template <int RPW, int NWV, int TGW, int TW, int NS, bool KV8, int HDIM>
+__global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) {
+  using P = PagedShape<RPW, NWV, TGW, TW, NS, KV8, HDIM>;
+  constexpr int NB = TW / 16, NKK = HDIM / 32, RB = P::RB, SB = P::SB, LPM = P::LPM, CPR = RB / 16, RPL = 1024 / RB;
+  constexpr int SRB = 2 * HDIM, NTH = 64 * P::NW, ROWS = P::ROWS, IDS = P::IDS;
+  constexpr bool KCONV = KV8 && NWV > 1;  // K and V converted once into shared bf16 tiles
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ float s_m[TGW][ROWS], s_l[TGW][ROWS];
+
+  const int lane = threadIdx.x & 63;
+  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tg = wid / NWV, wave = wid % NWV, rt0 = wave * RPW;
+  PagedItem it;
+  int S;
+  if (a.sp.single) {  // one split per KV head
+    it = PagedItem{(int)blockIdx.x / a.p.Hkv, (int)blockIdx.x % a.p.Hkv, 0, 1};
+    S = a.sp.fixed;
+  } else {
+    const int n0 = lane < a.p.B ? paged_span(a, paged_len(a.p, lane)).n : 0;
+    S = __builtin_amdgcn_readfirstlane(paged_split_blocks(a, n0));
+    if (!paged_locate(a, n0, S, blockIdx.x, it)) return;
+  }
+  const int b = __builtin_amdgcn_readfirstlane(it.b), g = __builtin_amdgcn_readfirstlane(it.g);
+  const int split = __builtin_amdgcn_readfirstlane(it.split), n_splits = __builtin_amdgcn_readfirstlane(it.n_splits);
+  const int Lv = __builtin_amdgcn_readfirstlane(paged_len(a.p, b));
+  const PagedSpan span = paged_span(a, Lv);
+  const int i0 = split * S;                                  // this split's blocks
+  const int n_blocks = max(0, min(span.n - i0, S));
+  const int all_tiles = (n_blocks + NB - 1) / NB;
+  const int ntiles = all_tiles > tg ? (all_tiles - tg + TGW - 1) / TGW : 0;  // tiles tg, tg + TGW, ...
+  const int min_pos = Lv - a.C;
+
+  uint4 q[RPW][NKK];
+  int rpos[RPW];
+#pragma unroll
+  for (int rr = 0; rr < RPW; ++rr) {
+    const int r = 16 * (rt0 + rr) + (lane & 15), c = r / a.Gp, h = r % a.Gp;
+    const bool real = c < a.C && h < a.G;
+    const uint16_t* p = a.q + (((int64_t)b * a.C + (real ? c : 0)) * a.Hq + g * a.G + (real ? h : 0)) * HDIM;
+#pragma unroll
+    for (int kk = 0; kk < NKK; ++kk) {
+      q[rr][kk] = *(const uint4*)(p + q_koff(kk, lane));
+      if (!real) q[rr][kk] = make_uint4(0, 0, 0, 0);
+    }
+    rpos[rr] = c < a.C ? Lv - a.C + c : Lv - 1;
+  }
+  const float c2 = KV8 ? a.c2 * a.k_scale[g] : a.c2;
+  const unsigned char* Kg = a.p.K + g * a.p.stride_h;
+  const unsigned char* Vg = a.p.V + g * a.p.stride_h;
+  unsigned char* ring_p = smem + tg * P::GB;
+  const uint32_t ring = lds_addr(ring_p);
+  unsigned char* tile_k = ring_p + NS * SB;   // KCONV: the converted tiles
+  unsigned char* tile_v = tile_k + TW * SRB;
+  int32_t* ids = (int32_t*)(smem + P::RING) + wid * IDS;
+
+  // page of the lane's block among the next 64 of this token group
+  auto fill_ids = [&](int tile) __attribute__((always_inline)) {
+    const int e = tile * NB + lane;                          // block of the group
+    const int i = ((e / NB) * TGW + tg) * NB + e % NB;       // block of the split
+    int id = -1;
+    if (i < n_blocks) {
+      id = a.p.table[(int64_t)b * a.p.max_pages + ((token_block(span, i0 + i) * 16) >> a.p.page_shift)];
+      if (!is_page(id, a.p.n_pages)) id = -1;
+    }
+    ids[e % IDS] = id;
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+  };
+  uint32_t lane_off[LPM];  // from a block's first row
+#pragma unroll
+  for (int u = 0; u < LPM; ++u) {
+    const int row = RPL * (wave * LPM + u) + lane / CPR;
+    lane_off[u] = (uint32_t)((row & 15) * (int)a.p.stride_t) +
+                  16u * (uint32_t)((lane % CPR) ^ (KV8 ? raw_swz<RB>(row) : stage_swz(row)));
+  }
+  // every stage issues all its loads (the waits count them): blocks that are
+  // none read page 0
+  auto issue = [&](int tile) __attribute__((always_inline)) {
+    if (tile % (IDS / 2 / NB) == 0) fill_ids(tile);
+    const uint32_t base = ring + (uint32_t)((tile % NS) * SB);
+    int64_t off[NB];
+#pragma unroll
+    for (int bi = 0; bi < NB; ++bi) {
+      const int id = max(0, __builtin_amdgcn_readfirstlane(ids[(tile * NB + bi) % IDS]));
+      const int t = 16 * token_block(span, i0 + (tile * TGW + tg) * NB + bi);
+      off[bi] = id * a.p.stride_p + (t & (a.p.page - 1)) * a.p.stride_t;
+    }
+#pragma unroll
+    for (int u = 0; u < LPM; ++u) {
+      const int n = wave * LPM + u, bi = (RPL * n) / 16;
+      const int64_t o = NB == 1 || bi == 0 ? off[0] : off[NB - 1];
+      dma16_s<false>(Kg + o, lane_off[u], __builtin_amdgcn_readfirstlane(base + 1024 * n));
+      dma16_s<false>(Vg + o, lane_off[u], __builtin_amdgcn_readfirstlane(base + TW * RB + 1024 * n));
     }
   };
-  float m = -INFINITY, l = 0.f;
-  for (int u = wave; u < n; u += NW) {
-    const int t = u < nf ? u : u - nf + w0;
-    const int id = a.p.table[(int64_t)b * a.p.max_pages + (t >> a.p.page_shift)];
-    if (!is_page(id, a.p.n_pages)) continue;
-    const int64_t off = id * a.p.stride_p + g * a.p.stride_h + (t & (a.p.page - 1)) * a.p.stride_t;
-    float k[EPL], v[EPL], s = 0.f;
-    load(a.p.K + off, k);
-    load(a.p.V + off, v);
+
+  WaveState<RPW, HDIM> st;
+  st.init();
+  // a group of one wave refills a stage as soon as it has read it; the waves
+  // of a shared ring meet once a stage, which leaves NS - 1 stages in flight
+  constexpr int AHEAD = NWV == 1 ? NS : NS - 1;
 #pragma unroll
-    for (int j = 0; j < EPL; ++j) s += q[j] * k[j];
+  for (int i = 0; i < AHEAD; ++i)
+    if (i < ntiles) issue(i);
+  for (int i = 0; i < ntiles; ++i) {
+    wait_ring<2 * LPM>(min(AHEAD - 1, ntiles - 1 - i));
+    asm volatile("" ::: "memory");
+    if constexpr (NWV > 1) {
+      __syncthreads();
+      if (i + AHEAD < ntiles) issue(i + AHEAD);
+    }
+    const unsigned char* stg = ring_p + (i % NS) * SB;
+    if constexpr (KCONV) {
+      convert_rows_e4m3<TW, 64 * NWV, HDIM>(stg, tile_k, 64 * wave + lane);
+      convert_rows_e4m3<TW, 64 * NWV, HDIM>(stg + TW * RB, tile_v, 64 * wave + lane);
+      __syncthreads();
+    }
+    int t0[NB];   // each block's first token, and whether it is there
+    bool there[NB], full = true;
 #pragma unroll
-    for (int w = 1; w < 64; w *= 2) s += __shfl_xor(s, w);
-    const float mn = fmaxf(m, s);
-    const float f = mn == -INFINITY ? 0.f : fast_exp2(m - mn), p = mn == -INFINITY ? 0.f : fast_exp2(s - mn);
-    m = mn;
-    l = l * f + p;
+    for (int bi = 0; bi < NB; ++bi) {
+      there[bi] = __builtin_amdgcn_readfirstlane(ids[(i * NB + bi) % IDS]) >= 0;
+      t0[bi] = 16 * token_block(span, i0 + (i * TGW + tg) * NB + bi);
+      full &= there[bi] && t0[bi] + 15 <= min_pos &&
+              (a.window == 0 || t0[bi] > Lv - 1 - a.window || t0[bi] + 15 < a.first);
+    }
+    f32x4 Sx[NB][RPW];
 #pragma unroll
-    for (int j = 0; j < EPL; ++j) o[j] = o[j] * f + p * v[j];
-  }
-  if (lane == 0) {
-    s_m[wave] = m;
-    s_l[wave] = l;
-  }
+    for (int bi = 0; bi < NB; ++bi) {
+      if constexpr (KCONV)
+        qk_block_swz<RPW>(tile_k, bi, q, Sx[bi], lane);
+      else if constexpr (KV8)
+        qk_block_e4m3<RPW, RB>(stg, bi, q, Sx[bi], lane);
+      else
+        qk_block_swz<RPW>(stg, bi, q, Sx[bi], lane);
+    }
+    auto seen_from = [&](int t, int pos) { return t <= pos && (a.window == 0 || t > pos - a.window || t < a.first); };
 #pragma unroll
-  for (int j = 0; j < EPL; ++j) s_o[wave][lane * EPL + j] = o[j];
-  __syncthreads();
-  const int d = threadIdx.x;
-  if (d >= HDIM) return;
-  const float sink = a.sink ? a.sink[h] * 1.4426950408889634f : -INFINITY;
-  float M = sink;
-  for (int w = 0; w < NW; ++w) M = fmaxf(M, s_m[w]);
-  float Z = 0.f, x = 0.f;
-  if (M != -INFINITY) {
-    Z = fast_exp2(sink - M);
-    for (int w = 0; w < NW; ++w) {
-      const float f = fast_exp2(s_m[w] - M);
-      Z += s_l[w] * f;
-      x += s_o[w][d] * f;
+    for (int bi = 0; bi < NB; ++bi)
+#pragma unroll
+      for (int rr = 0; rr < RPW; ++rr)
+#pragma unroll
+        for (int ii = 0; ii < 4; ++ii) {
+          float v = Sx[bi][rr][ii] * c2;
+          if (!full && !(there[bi] && seen_from(t0[bi] + 4 * (lane >> 4) + ii, rpos[rr]))) v = -INFINITY;
+          Sx[bi][rr][ii] = v;
+        }
+    PFrags<NB, RPW> pf;
+    paged_softmax(st, Sx, pf, lane);
+    const unsigned char* vt = KCONV ? tile_v : stg + TW * RB;
+    if (!full && any_not_finite<KV8, TW * RB>(stg + TW * RB, lane)) {
+      pv_per_query<RPW, NB, HDIM, KV8 && !KCONV, RB>(st, pf, vt, a.C, a.Gp, rt0, lane, [&](int bi, int j, int c) {
+        return there[bi] && seen_from(t0[bi] + 4 * (lane >> 4) + j, Lv - a.C + c);
+      });
+    } else {
+      if constexpr (KV8 && !KCONV)
+        pv_tile_e4m3<RPW, NB, HDIM, RB>(st, pf, vt, lane);
+      else
+        pv_tile<RPW, NB, HDIM>(st, pf, vt, lane);
+    }
+    if constexpr (NWV == 1) {
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the stage has been read
+      asm volatile("" ::: "memory");
+      if (i + NS < ntiles) issue(i + NS);
     }
   }
-  x *= (Z > 0.f ? 1.f / Z : 0.f) * (KV8 ? a.v_scale[g] : 1.f);
-  if (a.gate) x *= 1.f / (1.f + fast_exp2(-bf16_bits_to_f32(a.gate[orow * HDIM + d]) * 1.4426950408889634f));
-  a.out[orow * HDIM + d] = (uint16_t)pack_bf16x2(x, x);
+  if constexpr (NWV > 1 && TGW > 1)  // the other groups' barriers
+    for (int i = ntiles; i < (all_tiles + TGW - 1) / TGW; ++i) {
+      __syncthreads();
+      if (KCONV) __syncthreads();
+    }
+
+  // the groups' rows against their common maximum, summed; with one split the
+  // sink's logit takes part and the output is written
+  const bool whole = n_splits == 1;
+#pragma unroll
+  for (int rr = 0; rr < RPW; ++rr) {
+    const float l = sum_xor32(sum_xor16(st.l[rr]));
+    if (lane < 16) {
+      s_m[tg][16 * (rt0 + rr) + lane] = st.m[rr];
+      s_l[tg][16 * (rt0 + rr) + lane] = l;
+    }
+  }
+  const float v_scale = KV8 ? a.v_scale[g] : 1.f;
+  __syncthreads();  // and every ring is free
+  auto sink_of = [&](int r) {
+    const int h = r % a.Gp;
+    return whole && a.sink && h < a.G ? a.sink[g * a.G + h] * 1.4426950408889634f : -INFINITY;
+  };
+  auto row_max = [&](int r) {
+    float M = sink_of(r);
+#pragma unroll
+    for (int w = 0; w < TGW; ++w) M = fmaxf(M, s_m[w][r]);
+    return M;
+  };
+  constexpr int CW = P::CW, XS = CW + 4, NQ = CW / 4;
+  float* xo = (float*)smem;  // [TGW][ROWS][XS]
+#pragma unroll
+  for (int d0 = 0; d0 < HDIM; d0 += CW) {
+    if (d0) __syncthreads();
+#pragma unroll
+    for (int rr = 0; rr < RPW; ++rr)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = 16 * (rt0 + rr) + 4 * (lane >> 4) + i;
+        const float M = row_max(r);
+        const float f = merge_weight(s_m[tg][r], M);
+#pragma unroll
+        for (int nb = 0; nb < CW / 16; ++nb)
+          xo[(tg * ROWS + r) * XS + 16 * nb + (lane & 15)] = st.o[rr][d0 / 16 + nb][i] * f;
+      }
+    __syncthreads();
+    for (int e = threadIdx.x; e < ROWS * NQ; e += NTH) {
+      const int r = e / NQ, d = 4 * (e % NQ), c = r / a.Gp, h = r % a.Gp;
+      if (c >= a.C || h >= a.G) continue;
+      const float sink = sink_of(r), M = row_max(r);
+      float Z = merge_weight(sink, M);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < TGW; ++w) {
+        Z += s_l[w][r] * merge_weight(s_m[w][r], M);
+        const float4 x = *(const float4*)(xo + (w * ROWS + r) * XS + d);
+        o.x += x.x;
+        o.y += x.y;
+        o.z += x.z;
+        o.w += x.w;
+      }
+      if (whole) {
+        const int64_t at = (((int64_t)b * a.C + c) * a.Hq + g * a.G + h) * HDIM + d0 + d;
+        paged_store4(o, Z, v_scale, a.gate ? a.gate + at : nullptr, a.out + at);
+      } else {
+        const int64_t row = (int64_t)blockIdx.x * ROWS + r;
+        *(float4*)(a.part_o + row * HDIM + d0 + d) = o;
+        if (d0 + d == 0) *(float2*)(a.part_ml + 2 * row) = make_float2(M, Z);
+      }
+    }
+  }
+  if (!a.sp.single && split == 0 && threadIdx.x == 0)
+    *(int2*)(a.unit_items + 2 * ((int64_t)b * a.p.Hkv + g)) = make_int2(blockIdx.x, n_splits);
+}
+
+// Joins the splits' partial rows.  grid (row groups, B Hkv); NQ threads take a
+// row's column quads, SG such teams share a row's splits and meet in LDS.
+template <int HDIM, int SG>
+__global__ __launch_bounds__(NTP) void k_paged_merge(PagedAttnArgs a) {
+  constexpr int NQ = HDIM / 4, TEAMS = NTP / NQ, RPG = TEAMS / SG;  // rows per workgroup
+  __shared__ float s_m[TEAMS], s_l[TEAMS];
+  __shared__ float4 s_o[SG > 1 ? TEAMS : 1][NQ];
+  const int unit = blockIdx.y, g = unit % a.p.Hkv, b = unit / a.p.Hkv;
+  const int2 items = *(const int2*)(a.unit_items + 2 * (int64_t)unit);
+  if (items.y < 2) return;  // its one workgroup has written the output
+  const int team = threadIdx.x / NQ, dq = threadIdx.x % NQ;
+  const int r = blockIdx.x * RPG + team / SG, part = team % SG;
+  const bool real = r < a.C * a.G;
+  const int c = real ? r / a.G : 0, h = real ? r % a.G : 0;
+  const int64_t row0 = (int64_t)items.x * a.part_rows + c * a.Gp + h;
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  constexpr int U = 4;
+  for (int s0 = part; s0 < items.y; s0 += U * SG) {
+    float2 ml[U];
+    float4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = s0 + u * SG;
+      const int64_t row = row0 + (int64_t)min(s, items.y - 1) * a.part_rows;
+      ml[u] = *(const float2*)(a.part_ml + 2 * row);
+      x[u] = *(const float4*)(a.part_o + row * HDIM + 4 * dq);
+      if (s >= items.y) ml[u] = make_float2(-INFINITY, 0.f);
+    }
+    float mn = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) mn = fmaxf(mn, ml[u].x);
+    const float f = merge_weight(m, mn);
+    m = mn;
+    l *= f;
+    o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float w = merge_weight(ml[u].x, mn);
+      l += ml[u].y * w;
+      o.x += x[u].x * w;
+      o.y += x[u].y * w;
+      o.z += x[u].z * w;
+      o.w += x[u].w * w;
+    }
+  }
+  if constexpr (SG > 1) {
+    if (dq == 0) {
+      s_m[team] = m;
+      s_l[team] = l;
+    }
+    s_o[team][dq] = o;
+    __syncthreads();
+    if (part) return;
+    float M = m;
+#pragma unroll
+    for (int w = 1; w < SG; ++w) M = fmaxf(M, s_m[team + w]);
+    const float f = merge_weight(m, M);
+    l *= f;
+    o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+#pragma unroll
+    for (int w = 1; w < SG; ++w) {
+      const float e = merge_weight(s_m[team + w], M);
+      const float4 x = s_o[team + w][dq];
+      l += s_l[team + w] * e;
+      o.x += x.x * e;
+      o.y += x.y * e;
+      o.z += x.z * e;
+      o.w += x.w * e;
+    }
+    m = M;
+  }
+  if (!real) return;
+  if (a.sink) {
+    const float s = a.sink[g * a.G + h] * 1.4426950408889634f, M = fmaxf(m, s);
+    const float f = merge_weight(m, M);
+    l = l * f + merge_weight(s, M);
+    o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+  }
+  const int64_t at = (((int64_t)b * a.C + c) * a.Hq + g * a.G + h) * HDIM + 4 * dq;
+  paged_store4(o, l, a.v_scale ? a.v_scale[g] : 1.f, a.gate ? a.gate + at : nullptr, a.out + at);
 }
 
 // ============================================================================ append
@@ -489,15 +990,67 @@ __global__ __launch_bounds__(NTP) void k_pages_copy(PagesCopyArgs a) {
 }  // namespace
 
 // ============================================================================ host launchers
-hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s) {
-  const dim3 grid(a.Hq, a.C, a.p.B);
-#define HS2_PAGED_ATTN(kv8, hdim) k_paged_attn<kv8, hdim><<<grid, NTP, 0, s>>>(a)
-  if (a.k_scale) {
-    if (a.p.hd == 128) HS2_PAGED_ATTN(true, 128); else HS2_PAGED_ATTN(true, 256);
-  } else {
-    if (a.p.hd == 128) HS2_PAGED_ATTN(false, 128); else HS2_PAGED_ATTN(false, 256);
+// Shapes by query row tiles, cache format and head dim.  Columns: RT, E4M3, head
+// dim, row tiles per wave, waves per ring, token groups, rows and stages of a
+// ring.
+#define HS2_PAGED_SHAPES(X)                                            \
+  X(1, false, 128, 1, 1, 4, 16, 2) X(2, false, 128, 2, 1, 4, 16, 2)    \
+  X(4, false, 128, 2, 2, 2, 32, 2) X(8, false, 128, 2, 4, 1, 32, 2)    \
+  X(1, false, 256, 1, 1, 4, 16, 2) X(2, false, 256, 1, 2, 2, 16, 2)    \
+  X(4, false, 256, 1, 4, 1, 32, 2) X(8, false, 256, 1, 8, 1, 32, 2)    \
+  X(1, true, 128, 1, 1, 4, 32, 2) X(2, true, 128, 2, 1, 4, 32, 2)      \
+  X(4, true, 128, 2, 2, 2, 32, 2) X(8, true, 128, 2, 4, 1, 32, 2)      \
+  X(1, true, 256, 1, 1, 4, 16, 2) X(2, true, 256, 1, 2, 2, 16, 2)      \
+  X(4, true, 256, 1, 4, 1, 32, 2) X(8, true, 256, 1, 8, 1, 32, 2)
+
+PagedAttnShape paged_attn_shape(int RT, bool kv8, int hd) {
+#define HS2_PAGED_SHAPE(rt, f8, hdim, rpw, nwv, tgw, tw, ns)             \
+  if (RT == rt && kv8 == f8 && hd == hdim) {                             \
+    using P = PagedShape<rpw, nwv, tgw, tw, ns, f8, hdim>;               \
+    return PagedAttnShape{P::ROWS, tgw * tw / 16, P::WGS};               \
   }
-#undef HS2_PAGED_ATTN
+  HS2_PAGED_SHAPES(HS2_PAGED_SHAPE)
+#undef HS2_PAGED_SHAPE
+  return PagedAttnShape{0, 0, 0};
+}
+
+hipError_t set_paged_smem_limits() {
+  hipError_t e = hipSuccess;
+#define HS2_PAGED_ATTR(rt, f8, hdim, rpw, nwv, tgw, tw, ns)                                               \
+  if (e == hipSuccess)                                                                                    \
+    e = hipFuncSetAttribute((const void*)k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim>,                   \
+                            hipFuncAttributeMaxDynamicSharedMemorySize,                                   \
+                            PagedShape<rpw, nwv, tgw, tw, ns, f8, hdim>::LDS);
+  HS2_PAGED_SHAPES(HS2_PAGED_ATTR)
+#undef HS2_PAGED_ATTR
+  return e;
+}
+
+hipError_t launch_paged_attn(const PagedAttnArgs& a, int RT, hipStream_t s) {
+  const unsigned grid = a.sp.single ? a.p.B * a.p.Hkv : a.sp.n_items;
+  const bool kv8 = a.k_scale != nullptr;
+#define HS2_PAGED_LAUNCH(rt, f8, hdim, rpw, nwv, tgw, tw, ns)                                             \
+  if (RT == rt && kv8 == f8 && a.p.hd == hdim) {                                                          \
+    using P = PagedShape<rpw, nwv, tgw, tw, ns, f8, hdim>;                                                \
+    k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim><<<grid, 64 * P::NW, P::LDS, s>>>(a);                    \
+    return hipGetLastError();                                                                             \
+  }
+  HS2_PAGED_SHAPES(HS2_PAGED_LAUNCH)
+#undef HS2_PAGED_LAUNCH
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_paged_merge(const PagedAttnArgs& a, hipStream_t s) {
+  const int units = a.p.B * a.p.Hkv, rows = a.C * a.G;
+  const int teams = NTP / (a.p.hd / 4);
+  // a team per row where a KV head has few splits on average
+  const bool shared = a.sp.n_items > 8 * units;
+  const dim3 grid(shared ? rows : (rows + teams - 1) / teams, units);
+  if (a.p.hd == 128) {
+    if (shared) k_paged_merge<128, 8><<<grid, NTP, 0, s>>>(a); else k_paged_merge<128, 1><<<grid, NTP, 0, s>>>(a);
+  } else {
+    if (shared) k_paged_merge<256, 4><<<grid, NTP, 0, s>>>(a); else k_paged_merge<256, 1><<<grid, NTP, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 
