@@ -1103,6 +1103,13 @@ hs2_status paged_attn_impl(const hs2_paged_dims* d, const uint16_t* q, const voi
   a.Gp = next_pow2(a.G);
   a.window = window;
   a.first = first;
+  // rows that the last-level cache cannot hold until the next step stream past it
+  const int64_t row_bytes = 2 * (int64_t)d->head_dim * (kv8 ? 1 : 2);
+  const int64_t read = std::min((int64_t)d->n_pages * d->page * d->n_kv_heads,
+                                (int64_t)d->batch * d->n_kv_heads * plan.sp.cap_blocks * 16) * row_bytes;
+  a.stream = read > kLastLevelCacheBytes;
+  const int force_stream = env_int("HS2_PAGED_STREAM", -1);
+  if (force_stream == 0 || force_stream == 1) a.stream = force_stream;
   a.k_scale = k_scale;
   a.v_scale = v_scale;
   a.sink = sink;

@@ -206,6 +206,7 @@ struct PagedAttnArgs {
   float c2;                // softmax scale * log2(e)
   int C, Hq, G, Gp;
   int window, first;       // window 0: every token is seen
+  int stream;              // pool rows are read non-temporal
   const float* k_scale;    // [Hkv] for an E4M3 pool, else null
   const float* v_scale;
   const float* sink;       // [Hq] or null

@@ -44,11 +44,13 @@ __device__ inline bool is_page(int id, int n_pages) { return (uint32_t)id < (uin
 // The visible blocks of a sequence with Lv tokens.
 struct PagedSpan {
   int nf, w0, n;  // blocks of first tokens, first block of the window, all of them
+  int lo;         // the earliest token of any window
 };
 __device__ inline PagedSpan paged_span(const PagedAttnArgs& a, int Lv) {
   PagedSpan s;
   const int pos0 = max(0, Lv - a.C);  // the earliest query that sees anything
-  s.w0 = a.window > 0 ? max(0, pos0 - a.window + 1) / 16 : 0;
+  s.lo = a.window > 0 ? max(0, pos0 - a.window + 1) : 0;
+  s.w0 = s.lo / 16;
   s.nf = min((a.first + 15) / 16, s.w0);
   s.n = s.nf + (Lv + 15) / 16 - s.w0;
   return s;
@@ -257,7 +259,7 @@ struct PagedShape {
   static constexpr int LDS = RING + NW * IDS * 4;
   // workgroups per compute unit: each with its statistics and 1 KB to spare in 160 KB
   static constexpr int WGS = 160 * 1024 / (LDS + TGW * ROWS * 8 + 1024);
-  static_assert(LPM >= 1 && TW * RB == 1024 * LPM * NWV, "whole 1 KB loads for every wave and stage");
+  static_assert(LPM >= 1 && TW * RB == 1024 * LPM * NWV && TW <= 32, "whole 1 KB loads for every wave and stage, two blocks");
 };
 
 // Weight of a part with maximum m against the common maximum M (0 where it
@@ -279,7 +281,7 @@ __device__ inline void paged_store4(float4 o, float Z, float v_scale, const uint
   *(uint2*)out = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
 }
 
-template <int RPW, int NWV, int TGW, int TW, int NS, bool KV8, int HDIM>
+template <int RPW, int NWV, int TGW, int TW, int NS, bool KV8, int HDIM, bool NTL>
 __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) {
   using P = PagedShape<RPW, NWV, TGW, TW, NS, KV8, HDIM>;
   constexpr int NB = TW / 16, NKK = HDIM / 32, RB = P::RB, SB = P::SB, LPM = P::LPM, CPR = RB / 16, RPL = 1024 / RB;
@@ -347,31 +349,56 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
     asm volatile("" ::: "memory");
   };
+  // Tokens from a block's first on that some query sees lie in [lo, hi]: rows
+  // outside repeat one of them (not read from memory again, and no other
+  // garbage than a visible row's reaches the tile); of a block that is no
+  // page, row 0 of page 0 is read (the waits count every stage's loads).
+  struct Block {
+    int id, t0, lo, hi;
+  };
+  auto block_at = [&](int tile, int bi) __attribute__((always_inline)) {
+    Block k;
+    k.id = __builtin_amdgcn_readfirstlane(ids[(tile * NB + bi) % IDS]);
+    const int i = i0 + (tile * TGW + tg) * NB + bi;
+    k.t0 = 16 * token_block(span, i);
+    k.lo = k.id < 0 || k.t0 < a.first ? 0 : max(0, span.lo - k.t0);
+    k.hi = k.id < 0 ? 0 : min(15, (i < span.nf ? min(a.first, Lv) : Lv) - 1 - k.t0);
+    return k;
+  };
+  const int lrow = lane / CPR;  // this lane's row of a 1 KB load
+  auto lane_offset = [&](int row, int from) __attribute__((always_inline)) {
+    return (uint32_t)(from * (int)a.p.stride_t) +
+           16u * (uint32_t)((lane % CPR) ^ (KV8 ? raw_swz<RB>(row) : stage_swz(row)));
+  };
   uint32_t lane_off[LPM];  // from a block's first row
 #pragma unroll
   for (int u = 0; u < LPM; ++u) {
-    const int row = RPL * (wave * LPM + u) + lane / CPR;
-    lane_off[u] = (uint32_t)((row & 15) * (int)a.p.stride_t) +
-                  16u * (uint32_t)((lane % CPR) ^ (KV8 ? raw_swz<RB>(row) : stage_swz(row)));
+    const int row = RPL * (wave * LPM + u) + lrow;
+    lane_off[u] = lane_offset(row, row & 15);
   }
-  // every stage issues all its loads (the waits count them): blocks that are
-  // none read page 0
   auto issue = [&](int tile) __attribute__((always_inline)) {
     if (tile % (IDS / 2 / NB) == 0) fill_ids(tile);
     const uint32_t base = ring + (uint32_t)((tile % NS) * SB);
+    Block k[NB];
     int64_t off[NB];
+    bool all = true;
 #pragma unroll
     for (int bi = 0; bi < NB; ++bi) {
-      const int id = max(0, __builtin_amdgcn_readfirstlane(ids[(tile * NB + bi) % IDS]));
-      const int t = 16 * token_block(span, i0 + (tile * TGW + tg) * NB + bi);
-      off[bi] = id * a.p.stride_p + (t & (a.p.page - 1)) * a.p.stride_t;
+      k[bi] = block_at(tile, bi);
+      off[bi] = max(0, k[bi].id) * a.p.stride_p + (k[bi].id < 0 ? 0 : k[bi].t0 & (a.p.page - 1)) * a.p.stride_t;
+      all &= k[bi].lo == 0 && k[bi].hi == 15;
     }
 #pragma unroll
     for (int u = 0; u < LPM; ++u) {
       const int n = wave * LPM + u, bi = (RPL * n) / 16;
       const int64_t o = NB == 1 || bi == 0 ? off[0] : off[NB - 1];
-      dma16_s<false>(Kg + o, lane_off[u], __builtin_amdgcn_readfirstlane(base + 1024 * n));
-      dma16_s<false>(Vg + o, lane_off[u], __builtin_amdgcn_readfirstlane(base + TW * RB + 1024 * n));
+      uint32_t lo = lane_off[u];
+      if (!all) {
+        const int row = RPL * n + lrow, first = NB == 1 || bi == 0 ? k[0].lo : k[NB - 1].lo;
+        lo = lane_offset(row, max(first, min(row & 15, NB == 1 || bi == 0 ? k[0].hi : k[NB - 1].hi)));
+      }
+      dma16_s<NTL>(Kg + o, lo, __builtin_amdgcn_readfirstlane(base + 1024 * n));
+      dma16_s<NTL>(Vg + o, lo, __builtin_amdgcn_readfirstlane(base + TW * RB + 1024 * n));
     }
   };
 
@@ -396,12 +423,13 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
       convert_rows_e4m3<TW, 64 * NWV, HDIM>(stg + TW * RB, tile_v, 64 * wave + lane);
       __syncthreads();
     }
-    int t0[NB];   // each block's first token, and whether it is there
+    int t0[NB];  // each block's first token, and whether it is there
     bool there[NB], full = true;
 #pragma unroll
     for (int bi = 0; bi < NB; ++bi) {
-      there[bi] = __builtin_amdgcn_readfirstlane(ids[(i * NB + bi) % IDS]) >= 0;
-      t0[bi] = 16 * token_block(span, i0 + (i * TGW + tg) * NB + bi);
+      const Block k = block_at(i, bi);
+      there[bi] = k.id >= 0;
+      t0[bi] = k.t0;
       full &= there[bi] && t0[bi] + 15 <= min_pos &&
               (a.window == 0 || t0[bi] > Lv - 1 - a.window || t0[bi] + 15 < a.first);
     }
@@ -993,6 +1021,7 @@ __global__ __launch_bounds__(NTP) void k_pages_copy(PagesCopyArgs a) {
 // Shapes by query row tiles, cache format and head dim.  Columns: RT, E4M3, head
 // dim, row tiles per wave, waves per ring, token groups, rows and stages of a
 // ring.
+#ifndef HS2_PAGED_SHAPES
 #define HS2_PAGED_SHAPES(X)                                            \
   X(1, false, 128, 1, 1, 4, 16, 2) X(2, false, 128, 2, 1, 4, 16, 2)    \
   X(4, false, 128, 2, 2, 2, 32, 2) X(8, false, 128, 2, 4, 1, 32, 2)    \
@@ -1002,6 +1031,7 @@ __global__ __launch_bounds__(NTP) void k_pages_copy(PagesCopyArgs a) {
   X(4, true, 128, 2, 2, 2, 32, 2) X(8, true, 128, 2, 4, 1, 32, 2)      \
   X(1, true, 256, 1, 1, 4, 16, 2) X(2, true, 256, 1, 2, 2, 16, 2)      \
   X(4, true, 256, 1, 4, 1, 32, 2) X(8, true, 256, 1, 8, 1, 32, 2)
+#endif
 
 PagedAttnShape paged_attn_shape(int RT, bool kv8, int hd) {
 #define HS2_PAGED_SHAPE(rt, f8, hdim, rpw, nwv, tgw, tw, ns)             \
@@ -1014,13 +1044,19 @@ PagedAttnShape paged_attn_shape(int RT, bool kv8, int hd) {
   return PagedAttnShape{0, 0, 0};
 }
 
+template <int LDS>
+static hipError_t paged_allow_lds(const void* cached, const void* streamed) {
+  const hipError_t e = hipFuncSetAttribute(cached, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  return e != hipSuccess ? e : hipFuncSetAttribute(streamed, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+}
+
 hipError_t set_paged_smem_limits() {
   hipError_t e = hipSuccess;
 #define HS2_PAGED_ATTR(rt, f8, hdim, rpw, nwv, tgw, tw, ns)                                               \
   if (e == hipSuccess)                                                                                    \
-    e = hipFuncSetAttribute((const void*)k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim>,                   \
-                            hipFuncAttributeMaxDynamicSharedMemorySize,                                   \
-                            PagedShape<rpw, nwv, tgw, tw, ns, f8, hdim>::LDS);
+    e = paged_allow_lds<PagedShape<rpw, nwv, tgw, tw, ns, f8, hdim>::LDS>(                                \
+        (const void*)k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim, false>,                                \
+        (const void*)k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim, true>);
   HS2_PAGED_SHAPES(HS2_PAGED_ATTR)
 #undef HS2_PAGED_ATTR
   return e;
@@ -1032,7 +1068,10 @@ hipError_t launch_paged_attn(const PagedAttnArgs& a, int RT, hipStream_t s) {
 #define HS2_PAGED_LAUNCH(rt, f8, hdim, rpw, nwv, tgw, tw, ns)                                             \
   if (RT == rt && kv8 == f8 && a.p.hd == hdim) {                                                          \
     using P = PagedShape<rpw, nwv, tgw, tw, ns, f8, hdim>;                                                \
-    k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim><<<grid, 64 * P::NW, P::LDS, s>>>(a);                    \
+    if (a.stream)                                                                                         \
+      k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim, true><<<grid, 64 * P::NW, P::LDS, s>>>(a);            \
+    else                                                                                                  \
+      k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim, false><<<grid, 64 * P::NW, P::LDS, s>>>(a);           \
     return hipGetLastError();                                                                             \
   }
   HS2_PAGED_SHAPES(HS2_PAGED_LAUNCH)

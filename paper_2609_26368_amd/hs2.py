@@ -377,53 +377,69 @@ _I32 = (torch.int32,)
 _F32 = (torch.float32,)
 
 
-def _current(device):
-    """The kernels run on the current device: its tensors only."""
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors on the current HIP device expected, got {device}")
+# The kernels run on the current device and take its tensors only.  A check
+# costs 0.4 us a tensor, a launch 3: the checks below compare device indexes,
+# and word their refusal only when there is one (a call of the attention took
+# the host 9.2 us with _expect, of an append 10.5).
+def _current():
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else torch.cuda.current_device()
 
 
-def _check_pool(dims, K, V, device, fp8):
-    dtypes, what = (_FP8, "E4M3 (uint8)") if fp8 else (_BF16, "bf16")
+def _take(t, name, shape, dtypes, index):
+    """Address of a contiguous tensor of this shape, type and device."""
+    if t.shape != shape or t.dtype not in dtypes or t.get_device() != index or not t.is_contiguous():
+        _expect(t, name, shape, dtypes, torch.device("cuda", index))
+        raise ValueError(f"{name}: a tensor on the current HIP device expected")
+    return t.data_ptr()
+
+
+def _take_pool(dims, K, V, index, fp8):
+    dtypes = _FP8 if fp8 else _BF16
     last = ((dims.n_pages - 1) * dims.kv_stride_p + (dims.n_kv_heads - 1) * dims.kv_stride_h
             + (dims.page - 1) * dims.kv_stride_t + dims.head_dim)
     for name, t in (("K", K), ("V", V)):
-        if t.dtype not in dtypes or t.device != device:
-            raise ValueError(f"{name}: {what} tensor on {device} expected")
-        avail = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
-        if last > avail:
-            raise ValueError(f"{name}: strides address {last} elements, storage holds {avail}")
+        if t.dtype not in dtypes or t.get_device() != index:
+            raise ValueError(f"{name}: {'E4M3 (uint8)' if fp8 else 'bf16'} tensor on the current HIP device expected")
+        if (t.storage_offset() + last) * (1 if fp8 else 2) > t.untyped_storage().nbytes():
+            raise ValueError(f"{name}: strides address {last} elements, more than the storage holds")
+    return K.data_ptr(), V.data_ptr()
 
 
-def _workspace(workspace, device):
-    if workspace is None or workspace.device != device or not workspace.is_contiguous():
-        raise ValueError(f"workspace: a contiguous tensor on {device} is required")
+def _take_scales(dims, scales, index):
+    shape = (dims.n_kv_heads,)
+    return [_take(scales[0], "k_scale", shape, _F32, index), _take(scales[1], "v_scale", shape, _F32, index)]
+
+
+def _take_workspace(workspace, index):
+    if workspace is None or workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor on the current HIP device is required")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
+def _stream_on(stream, index):
+    return torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream)
+
+
 def _paged_attn(dims, q, K, V, scales, table, len, span, sink, gate, out, workspace, stream):
-    dev = q.device
-    _current(dev)
-    B, C, Hq, D = dims.batch, dims.n_queries, dims.n_q_heads, dims.head_dim
-    shape = (B, C, Hq, D)
-    _expect(q, "q", shape, _BF16, dev)
-    _check_pool(dims, K, V, dev, scales is not None)
+    index = _current()
+    B, Hq = dims.batch, dims.n_q_heads
+    shape = (B, dims.n_queries, Hq, dims.head_dim)
+    args = [_take(q, "q", shape, _BF16, index), *_take_pool(dims, K, V, index, scales is not None)]
     if scales is not None:
-        _check_scales(dims, scales[0], scales[1], dev)
-    _expect(table, "table", (B, dims.max_pages), _I32, dev)
-    _expect(len, "len", (B,), _I32, dev)
-    if sink is not None:
-        _expect(sink, "sink", (Hq,), _F32, dev)
-    if gate is not None:
-        _expect(gate, "gate", shape, _BF16, dev)
-    _expect(out, "out", shape, _BF16, dev)
-    ws, ws_bytes = _workspace(workspace, dev)
-    name = "hs2_paged_attn" if span is None else "hs2_paged_window_attn"
-    call = getattr(load(), name if scales is None else name + "_fp8")
-    args = [] if scales is None else [_ptr(scales[0]), _ptr(scales[1])]
-    span = () if span is None else (int(span[0]), int(span[1]))
-    _check(call(ctypes.byref(dims), _ptr(q), _ptr(K), _ptr(V), *args, _ptr(table), _ptr(len), *span, _ptr(sink),
-                _ptr(gate), _ptr(out), ws, ws_bytes, _stream(stream)))
+        args += _take_scales(dims, scales, index)
+    args.append(_take(table, "table", (B, dims.max_pages), _I32, index))
+    args.append(_take(len, "len", (B,), _I32, index))
+    if span is not None:
+        args += (int(span[0]), int(span[1]))
+    args.append(None if sink is None else _take(sink, "sink", (Hq,), _F32, index))
+    args.append(None if gate is None else _take(gate, "gate", shape, _BF16, index))
+    args.append(_take(out, "out", shape, _BF16, index))
+    lib = load()
+    if span is None:
+        call = lib.hs2_paged_attn if scales is None else lib.hs2_paged_attn_fp8
+    else:
+        call = lib.hs2_paged_window_attn if scales is None else lib.hs2_paged_window_attn_fp8
+    _check(call(ctypes.byref(dims), *args, *_take_workspace(workspace, index), _stream_on(stream, index)))
 
 
 def hs2_paged_attn(dims, q, K, V, table, len, sink, gate, out, workspace, stream=None):
@@ -449,28 +465,25 @@ def hs2_paged_window_attn_fp8(dims, q, K8, V8, k_scale, v_scale, table, len, win
 
 
 def _paged_append(dims, k_new, v_new, n_new, scales, table, len, K, V, stream):
-    dev = k_new.device
-    _current(dev)
+    index = _current()
     B, Hkv, D = dims.batch, dims.n_kv_heads, dims.head_dim
+    shape, strides = k_new.shape, k_new.stride()
+    if k_new.dim() != 4 or (shape[0], shape[2], shape[3]) != (B, Hkv, D) or shape[1] < 1:
+        raise ValueError(f"k_new: shape {tuple(shape)}, expected ({B}, tokens, {Hkv}, {D})")
+    if v_new.shape != shape or v_new.stride() != strides or strides[3] != 1:
+        raise ValueError("k_new and v_new: one shape and one set of strides, rows of contiguous elements expected")
     for name, t in (("k_new", k_new), ("v_new", v_new)):
-        if t.dim() != 4 or (t.shape[0], t.shape[2], t.shape[3]) != (B, Hkv, D) or t.shape[1] < 1:
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected ({B}, tokens, {Hkv}, {D})")
-        if t.dtype not in _BF16 or t.device != dev or t.stride(3) != 1:
-            raise ValueError(f"{name}: bf16 rows of contiguous elements on {dev} expected")
-    if k_new.shape != v_new.shape or k_new.stride() != v_new.stride():
-        raise ValueError("k_new and v_new: one shape and one set of strides expected")
-    if n_new is not None:
-        _expect(n_new, "n_new", (B,), _I32, dev)
-    _check_pool(dims, K, V, dev, scales is not None)
+        if t.dtype not in _BF16 or t.get_device() != index:
+            raise ValueError(f"{name}: bf16 tensor on the current HIP device expected")
+    args = [k_new.data_ptr(), v_new.data_ptr(), *strides[:3], shape[1],
+            None if n_new is None else _take(n_new, "n_new", (B,), _I32, index)]
     if scales is not None:
-        _check_scales(dims, scales[0], scales[1], dev)
-    _expect(table, "table", (B, dims.max_pages), _I32, dev)
-    _expect(len, "len", (B,), _I32, dev)
-    sb, st, sh, _ = k_new.stride()
+        args += _take_scales(dims, scales, index)
+    args.append(_take(table, "table", (B, dims.max_pages), _I32, index))
+    args.append(_take(len, "len", (B,), _I32, index))
     call = load().hs2_paged_append if scales is None else load().hs2_paged_append_fp8
-    args = [] if scales is None else [_ptr(scales[0]), _ptr(scales[1])]
-    _check(call(ctypes.byref(dims), _ptr(k_new), _ptr(v_new), sb, st, sh, k_new.shape[1], _ptr(n_new), *args,
-                _ptr(table), _ptr(len), _ptr(K), _ptr(V), _stream(stream)))
+    _check(call(ctypes.byref(dims), *args, *_take_pool(dims, K, V, index, scales is not None),
+                _stream_on(stream, index)))
 
 
 def hs2_paged_append(dims, k_new, v_new, n_new, table, len, K, V, stream=None):
@@ -484,65 +497,59 @@ def hs2_paged_append_fp8(dims, k_new, v_new, n_new, k_scale, v_scale, table, len
     _paged_append(dims, k_new, v_new, n_new, (k_scale, v_scale), table, len, K8, V8, stream)
 
 
-def _pages(dims, table, refs, table_out, refs_out, counts, workspace):
-    dev = table.device
-    _current(dev)
-    shape = (dims.batch, dims.max_pages)
-    _expect(table, "table", shape, _I32, dev)
-    _expect(table_out, "table_out", shape, _I32, dev)
-    _expect(refs, "refs", (dims.n_pages,), _I32, dev)
-    _expect(refs_out, "refs_out", (dims.n_pages,), _I32, dev)
-    _expect(counts, "counts", (2,), _I32, dev)
-    return dev, *_workspace(workspace, dev)
-
-
-def _expect_moves(moves, least, device):
+def _take_moves(moves, least, index):
     if moves.dim() != 2 or moves.shape[0] < least:
         raise ValueError(f"moves: shape {tuple(moves.shape)}, at least ({least}, 3) expected")
-    _expect(moves, "moves", (moves.shape[0], 3), _I32, device)
+    return _take(moves, "moves", (moves.shape[0], 3), _I32, index), moves.shape[0]
 
 
 def hs2_pages_extend(dims, table, len, refs, table_out, refs_out, counts, workspace, stream=None):
     """Free pages for every row that holds fewer than len[b] tokens need; table_out and refs_out may be the inputs."""
-    dev, ws, ws_bytes = _pages(dims, table, refs, table_out, refs_out, counts, workspace)
-    _expect(len, "len", (dims.batch,), _I32, dev)
-    _check(load().hs2_pages_extend(ctypes.byref(dims), _ptr(table), _ptr(len), _ptr(refs), _ptr(table_out),
-                                   _ptr(refs_out), _ptr(counts), ws, ws_bytes, _stream(stream)))
+    index, B, pool = _current(), dims.batch, (dims.n_pages,)
+    shape = (B, dims.max_pages)
+    _check(load().hs2_pages_extend(
+        ctypes.byref(dims), _take(table, "table", shape, _I32, index), _take(len, "len", (B,), _I32, index),
+        _take(refs, "refs", pool, _I32, index), _take(table_out, "table_out", shape, _I32, index),
+        _take(refs_out, "refs_out", pool, _I32, index), _take(counts, "counts", (2,), _I32, index),
+        *_take_workspace(workspace, index), _stream_on(stream, index)))
 
 
 def hs2_pages_reorder(dims, parent, table, len, refs, table_out, len_out, refs_out, moves, counts, workspace,
                       stream=None):
     """Every row takes over its parent row's tokens (a fork, a permutation; a parent outside [0, B) frees the row);
     hs2_pages_copy has to copy the moves in every layer's pool."""
-    dev, ws, ws_bytes = _pages(dims, table, refs, table_out, refs_out, counts, workspace)
-    for name, t in (("parent", parent), ("len", len), ("len_out", len_out)):
-        _expect(t, name, (dims.batch,), _I32, dev)
-    _expect_moves(moves, dims.batch, dev)
-    _check(load().hs2_pages_reorder(ctypes.byref(dims), _ptr(parent), _ptr(table), _ptr(len), _ptr(refs),
-                                    _ptr(table_out), _ptr(len_out), _ptr(refs_out), _ptr(moves), moves.shape[0],
-                                    _ptr(counts), ws, ws_bytes, _stream(stream)))
+    index, rows, pool = _current(), (dims.batch,), (dims.n_pages,)
+    shape = (dims.batch, dims.max_pages)
+    _check(load().hs2_pages_reorder(
+        ctypes.byref(dims), _take(parent, "parent", rows, _I32, index), _take(table, "table", shape, _I32, index),
+        _take(len, "len", rows, _I32, index), _take(refs, "refs", pool, _I32, index),
+        _take(table_out, "table_out", shape, _I32, index), _take(len_out, "len_out", rows, _I32, index),
+        _take(refs_out, "refs_out", pool, _I32, index), *_take_moves(moves, dims.batch, index),
+        _take(counts, "counts", (2,), _I32, index), *_take_workspace(workspace, index), _stream_on(stream, index)))
 
 
 def hs2_pages_compact(dims, table, refs, table_out, refs_out, moves, counts, workspace, stream=None):
     """Packs the used pages to the front of the pool; hs2_pages_copy has to copy the moves in every layer's pool."""
-    dev, ws, ws_bytes = _pages(dims, table, refs, table_out, refs_out, counts, workspace)
-    _expect_moves(moves, max(1, dims.n_pages // 2), dev)
-    _check(load().hs2_pages_compact(ctypes.byref(dims), _ptr(table), _ptr(refs), _ptr(table_out), _ptr(refs_out),
-                                    _ptr(moves), moves.shape[0], _ptr(counts), ws, ws_bytes, _stream(stream)))
+    index, pool = _current(), (dims.n_pages,)
+    shape = (dims.batch, dims.max_pages)
+    _check(load().hs2_pages_compact(
+        ctypes.byref(dims), _take(table, "table", shape, _I32, index), _take(refs, "refs", pool, _I32, index),
+        _take(table_out, "table_out", shape, _I32, index), _take(refs_out, "refs_out", pool, _I32, index),
+        *_take_moves(moves, max(1, dims.n_pages // 2), index), _take(counts, "counts", (2,), _I32, index),
+        *_take_workspace(workspace, index), _stream_on(stream, index)))
 
 
 def hs2_pages_copy(dims, moves, n_moves, K, V, stream=None):
     """Copies the first n_moves[0] moves (int32 on the device, as the calls above leave it) in one layer's pool."""
-    dev = K.device
-    _current(dev)
-    _expect_moves(moves, 0, dev)
-    if n_moves.dtype != torch.int32 or n_moves.device != dev or n_moves.numel() < 1:
-        raise ValueError(f"n_moves: int32 on {dev} expected")
+    index = _current()
+    if n_moves.dtype != torch.int32 or n_moves.get_device() != index or n_moves.numel() < 1:
+        raise ValueError("n_moves: int32 on the current HIP device expected")
+    at, most = _take_moves(moves, 0, index)
     fp8 = K.dtype in _FP8
-    _check_pool(dims, K, V, dev, fp8)
-    if moves.shape[0]:
-        _check(load().hs2_pages_copy(ctypes.byref(dims), _ptr(moves), _ptr(n_moves), moves.shape[0], 1 if fp8 else 2,
-                                     _ptr(K), _ptr(V), _stream(stream)))
+    pool = _take_pool(dims, K, V, index, fp8)
+    if most:
+        _check(load().hs2_pages_copy(ctypes.byref(dims), at, n_moves.data_ptr(), most, 1 if fp8 else 2, *pool,
+                                     _stream_on(stream, index)))
 
 
 STREAM_PROBE_SINK_WORDS = 4096
