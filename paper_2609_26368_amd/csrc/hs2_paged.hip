@@ -40,6 +40,17 @@ __device__ inline bool is_page(int id, int n_pages) { return (uint32_t)id < (uin
 // share its tiles, RPW row tiles of 16 query rows each.  A group of one wave
 // needs no barrier.  The groups meet in LDS; a KV head of one split is
 // finished there, of more it leaves partial rows for k_paged_merge.
+//
+// What a query does not see must not reach it, and 0 x NaN is NaN: rows that no
+// query sees are never loaded (they repeat a visible row of their block, or are
+// zero rows), and the few tiles of which the queries see different rows (the
+// last tokens of a chunk, the starts of its windows) are left to a second loop.
+// In the loop itself all rows of a tile are seen by every query or by none;
+// with both products in one loop the compiler kept O twice (154 registers a
+// lane for one row tile of head dim 128).
+
+// What stands in for rows that are not loaded.
+__device__ const uint4 zero_row[32] = {};
 
 // The visible blocks of a sequence with Lv tokens.
 struct PagedSpan {
@@ -201,23 +212,30 @@ __device__ inline uint4 v_operand(const unsigned char* v, int i, int nb, int lan
   }
 }
 
-// O += P V of a tile in which some rows are hidden from some queries and some
-// V is not finite: a product with a probability of 0 would still carry a NaN
-// into the rows of the queries that do not see it.  One pass per query, with
-// the rows that it does not see taken as 0, kept in that query's rows only.
-// seen(t4, j, c): whether query c sees token t4 + j of the lane's four.
+// O += P V of a tile of which the queries see different rows.  Where some V is
+// not finite (apart), a product with a probability of 0 would carry a NaN into
+// the rows of the queries that do not see it: then one pass per query, with the
+// rows that it does not see taken as 0, kept in that query's rows only.
+// seen(bi, j, c): whether query c sees the lane's token j of block bi.
 template <int RPW, int NB, int HDIM, bool KV8, int RB, class Seen>
-__device__ inline void pv_per_query(WaveState<RPW, HDIM>& st, const PFrags<NB, RPW>& pf, const unsigned char* v, int C,
-                                    int Gp, int rt0, int lane, Seen&& seen) {
+__device__ inline void pv_apart(WaveState<RPW, HDIM>& st, const PFrags<NB, RPW>& pf, const unsigned char* v, bool apart,
+                                int C, int Gp, int rt0, int lane, Seen&& seen) {
   constexpr bool K32 = NB % 2 == 0;
-  for (int c = 0; c < C; ++c) {
+  int c = 0;
+  do {
+    uint32_t mine[RPW][4];  // the rows of query c
+#pragma unroll
+    for (int rr = 0; rr < RPW; ++rr)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        mine[rr][k] = !apart || (16 * (rt0 + rr) + 4 * (lane >> 4) + k) / Gp == c ? 0xFFFFFFFFu : 0u;
 #pragma unroll
     for (int i = 0; i < (K32 ? NB / 2 : NB); ++i) {
       uint32_t keep[4];  // of the lane's tokens, two a word, in the operand's order
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int bi = K32 ? 2 * i + (j >> 1) : i, t = 2 * (j & 1);
-        keep[j] = (seen(bi, t, c) ? 0xFFFFu : 0u) | (seen(bi, t + 1, c) ? 0xFFFF0000u : 0u);
+        keep[j] = (!apart || seen(bi, t, c) ? 0xFFFFu : 0u) | (!apart || seen(bi, t + 1, c) ? 0xFFFF0000u : 0u);
       }
 #pragma unroll
       for (int nb = 0; nb < HDIM / 16; ++nb) {
@@ -235,11 +253,12 @@ __device__ inline void pv_per_query(WaveState<RPW, HDIM>& st, const PFrags<NB, R
             d = mfma_k16(pf.h[i][rr], make_uint2(x.x, x.y), d);
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            if ((16 * (rt0 + rr) + 4 * (lane >> 4) + k) / Gp == c) st.o[rr][nb][k] += d[k];
+            st.o[rr][nb][k] += __uint_as_float(__float_as_uint(d[k]) & mine[rr][k]);
         }
+        __builtin_amdgcn_sched_barrier(0);  // one operand at a time: a rare loop is not to cost the other registers
       }
     }
-  }
+  } while (apart && ++c < C);
 }
 
 // Shapes: LDS of a workgroup and what follows from the template's numbers.
@@ -310,11 +329,11 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
   const int i0 = split * S;                                  // this split's blocks
   const int n_blocks = max(0, min(span.n - i0, S));
   const int all_tiles = (n_blocks + NB - 1) / NB;
-  const int ntiles = all_tiles > tg ? (all_tiles - tg + TGW - 1) / TGW : 0;  // tiles tg, tg + TGW, ...
-  const int min_pos = Lv - a.C;
+  // tiles tg, tg + TGW, ...; a group without one takes a tile of zero rows, so
+  // that the loop always runs (see below)
+  const int ntiles = max(1, (all_tiles - tg + TGW - 1) / TGW);
 
   uint4 q[RPW][NKK];
-  int rpos[RPW];
 #pragma unroll
   for (int rr = 0; rr < RPW; ++rr) {
     const int r = 16 * (rt0 + rr) + (lane & 15), c = r / a.Gp, h = r % a.Gp;
@@ -325,7 +344,6 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
       q[rr][kk] = *(const uint4*)(p + q_koff(kk, lane));
       if (!real) q[rr][kk] = make_uint4(0, 0, 0, 0);
     }
-    rpos[rr] = c < a.C ? Lv - a.C + c : Lv - 1;
   }
   const float c2 = KV8 ? a.c2 * a.k_scale[g] : a.c2;
   const unsigned char* Kg = a.p.K + g * a.p.stride_h;
@@ -349,20 +367,39 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
     asm volatile("" ::: "memory");
   };
-  // Tokens from a block's first on that some query sees lie in [lo, hi]: rows
-  // outside repeat one of them (not read from memory again, and no other
-  // garbage than a visible row's reaches the tile); of a block that is no
-  // page, row 0 of page 0 is read (the waits count every stage's loads).
+  // Tiles of which the queries see different rows: those with the starts of the
+  // later queries' windows (or where first tokens end and a window begins in
+  // one block) and those with the chunk's own tokens.
+  int a0 = 0, a1 = -1, e0 = 0, e1 = -1;
+  {
+    const bool gap = a.window > 0 && (a.first + 15) / 16 > span.w0 && a.first < span.lo;
+    const int last = a.window > 0 ? Lv - 1 - a.window : -1;  // the last token that the last query does not see any more
+    auto tile_of = [&](int block) { return (block - span.w0 + span.nf - i0) >> (NB - 1); };  // rounded down
+    if (n_blocks > 0 && (gap || (a.C > 1 && last >= span.lo))) {
+      a0 = max(0, tile_of(span.w0));
+      a1 = min(all_tiles - 1, tile_of(max(span.w0, last >= 0 ? last / 16 : 0)));
+    }
+    if (n_blocks > 0 && a.C > 1) {
+      e0 = max(0, tile_of(max(0, Lv - a.C + 1) / 16));
+      e1 = min(all_tiles - 1, tile_of((Lv - 1) / 16));
+    }
+  }
+  auto is_apart = [&](int T) { return (T >= a0 && T <= a1) || (T >= e0 && T <= e1); };
+
+  // A block's page and first token; the rows [lo, hi] of it are seen by some
+  // query (rows outside repeat one of them).  zero: of no row.
   struct Block {
     int id, t0, lo, hi;
+    bool zero;
   };
-  auto block_at = [&](int tile, int bi) __attribute__((always_inline)) {
+  auto block_at = [&](int tile, int bi, bool apart) __attribute__((always_inline)) {
     Block k;
     k.id = __builtin_amdgcn_readfirstlane(ids[(tile * NB + bi) % IDS]);
     const int i = i0 + (tile * TGW + tg) * NB + bi;
     k.t0 = 16 * token_block(span, i);
-    k.lo = k.id < 0 || k.t0 < a.first ? 0 : max(0, span.lo - k.t0);
-    k.hi = k.id < 0 ? 0 : min(15, (i < span.nf ? min(a.first, Lv) : Lv) - 1 - k.t0);
+    k.zero = k.id < 0 || apart;
+    k.lo = k.t0 < a.first ? 0 : max(0, span.lo - k.t0);
+    k.hi = min(15, (i < span.nf ? min(a.first, Lv) : Lv) - 1 - k.t0);
     return k;
   };
   const int lrow = lane / CPR;  // this lane's row of a 1 KB load
@@ -376,29 +413,55 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
     const int row = RPL * (wave * LPM + u) + lrow;
     lane_off[u] = lane_offset(row, row & 15);
   }
-  auto issue = [&](int tile) __attribute__((always_inline)) {
-    if (tile % (IDS / 2 / NB) == 0) fill_ids(tile);
-    const uint32_t base = ring + (uint32_t)((tile % NS) * SB);
-    Block k[NB];
-    int64_t off[NB];
+  // (every stage issues all its loads: the waits count them)
+  auto issue_as = [&](int tile, int stage, const Block (&k)[NB]) __attribute__((always_inline)) {
+    const uint32_t base = ring + (uint32_t)(stage * SB);
+    const unsigned char *kp[NB], *vp[NB];
     bool all = true;
 #pragma unroll
     for (int bi = 0; bi < NB; ++bi) {
-      k[bi] = block_at(tile, bi);
-      off[bi] = max(0, k[bi].id) * a.p.stride_p + (k[bi].id < 0 ? 0 : k[bi].t0 & (a.p.page - 1)) * a.p.stride_t;
-      all &= k[bi].lo == 0 && k[bi].hi == 15;
+      const int64_t off = k[bi].id * a.p.stride_p + (k[bi].t0 & (a.p.page - 1)) * a.p.stride_t;
+      kp[bi] = k[bi].zero ? (const unsigned char*)zero_row : Kg + off;
+      vp[bi] = k[bi].zero ? (const unsigned char*)zero_row : Vg + off;
+      all &= !k[bi].zero && k[bi].lo == 0 && k[bi].hi == 15;
     }
 #pragma unroll
     for (int u = 0; u < LPM; ++u) {
-      const int n = wave * LPM + u, bi = (RPL * n) / 16;
-      const int64_t o = NB == 1 || bi == 0 ? off[0] : off[NB - 1];
+      const int n = wave * LPM + u;
+      const bool second = NB > 1 && (RPL * n) / 16 == 1;
       uint32_t lo = lane_off[u];
       if (!all) {
-        const int row = RPL * n + lrow, first = NB == 1 || bi == 0 ? k[0].lo : k[NB - 1].lo;
-        lo = lane_offset(row, max(first, min(row & 15, NB == 1 || bi == 0 ? k[0].hi : k[NB - 1].hi)));
+        const int row = RPL * n + lrow;
+        const int from = max(second ? k[NB - 1].lo : k[0].lo, min(row & 15, second ? k[NB - 1].hi : k[0].hi));
+        lo = lane_offset(row, (second ? k[NB - 1].zero : k[0].zero) ? 0 : from);
       }
-      dma16_s<NTL>(Kg + o, lo, __builtin_amdgcn_readfirstlane(base + 1024 * n));
-      dma16_s<NTL>(Vg + o, lo, __builtin_amdgcn_readfirstlane(base + TW * RB + 1024 * n));
+      dma16_s<NTL>(second ? kp[NB - 1] : kp[0], lo, __builtin_amdgcn_readfirstlane(base + 1024 * n));
+      dma16_s<NTL>(second ? vp[NB - 1] : vp[0], lo, __builtin_amdgcn_readfirstlane(base + TW * RB + 1024 * n));
+    }
+  };
+  auto issue = [&](int tile) __attribute__((always_inline)) {
+    if (tile % (IDS / 2 / NB) == 0) fill_ids(tile);
+    Block k[NB];
+#pragma unroll
+    for (int bi = 0; bi < NB; ++bi) k[bi] = block_at(tile, bi, is_apart(tile * TGW + tg));
+    issue_as(tile, tile % NS, k);
+  };
+  auto logits = [&](const unsigned char* stg, f32x4 (&Sx)[NB][RPW]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int bi = 0; bi < NB; ++bi) {
+      if constexpr (KCONV)
+        qk_block_swz<RPW>(tile_k, bi, q, Sx[bi], lane);
+      else if constexpr (KV8)
+        qk_block_e4m3<RPW, RB>(stg, bi, q, Sx[bi], lane);
+      else
+        qk_block_swz<RPW>(stg, bi, q, Sx[bi], lane);
+    }
+  };
+  auto convert = [&](const unsigned char* stg) __attribute__((always_inline)) {
+    if constexpr (KCONV) {
+      convert_rows_e4m3<TW, 64 * NWV, HDIM>(stg, tile_k, 64 * wave + lane);
+      convert_rows_e4m3<TW, 64 * NWV, HDIM>(stg + TW * RB, tile_v, 64 * wave + lane);
+      __syncthreads();
     }
   };
 
@@ -410,6 +473,7 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i)
     if (i < ntiles) issue(i);
+  __builtin_assume(ntiles >= 1);
   for (int i = 0; i < ntiles; ++i) {
     wait_ring<2 * LPM>(min(AHEAD - 1, ntiles - 1 - i));
     asm volatile("" ::: "memory");
@@ -418,55 +482,40 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
       if (i + AHEAD < ntiles) issue(i + AHEAD);
     }
     const unsigned char* stg = ring_p + (i % NS) * SB;
-    if constexpr (KCONV) {
-      convert_rows_e4m3<TW, 64 * NWV, HDIM>(stg, tile_k, 64 * wave + lane);
-      convert_rows_e4m3<TW, 64 * NWV, HDIM>(stg + TW * RB, tile_v, 64 * wave + lane);
-      __syncthreads();
-    }
-    int t0[NB];  // each block's first token, and whether it is there
-    bool there[NB], full = true;
-#pragma unroll
-    for (int bi = 0; bi < NB; ++bi) {
-      const Block k = block_at(i, bi);
-      there[bi] = k.id >= 0;
-      t0[bi] = k.t0;
-      full &= there[bi] && t0[bi] + 15 <= min_pos &&
-              (a.window == 0 || t0[bi] > Lv - 1 - a.window || t0[bi] + 15 < a.first);
-    }
+    convert(stg);
     f32x4 Sx[NB][RPW];
+    logits(stg, Sx);
+    int lo[NB], hi[NB];  // rows that the queries see
+    bool full = true;
 #pragma unroll
     for (int bi = 0; bi < NB; ++bi) {
-      if constexpr (KCONV)
-        qk_block_swz<RPW>(tile_k, bi, q, Sx[bi], lane);
-      else if constexpr (KV8)
-        qk_block_e4m3<RPW, RB>(stg, bi, q, Sx[bi], lane);
-      else
-        qk_block_swz<RPW>(stg, bi, q, Sx[bi], lane);
+      const Block k = block_at(i, bi, is_apart(i * TGW + tg));
+      lo[bi] = k.lo;
+      hi[bi] = k.zero ? -1 : k.hi;
+      full &= lo[bi] == 0 && hi[bi] == 15;
     }
-    auto seen_from = [&](int t, int pos) { return t <= pos && (a.window == 0 || t > pos - a.window || t < a.first); };
 #pragma unroll
     for (int bi = 0; bi < NB; ++bi)
 #pragma unroll
-      for (int rr = 0; rr < RPW; ++rr)
+      for (int rr = 0; rr < RPW; ++rr) Sx[bi][rr] *= c2;
+    if (!full) {
+#pragma unroll
+      for (int bi = 0; bi < NB; ++bi)
 #pragma unroll
         for (int ii = 0; ii < 4; ++ii) {
-          float v = Sx[bi][rr][ii] * c2;
-          if (!full && !(there[bi] && seen_from(t0[bi] + 4 * (lane >> 4) + ii, rpos[rr]))) v = -INFINITY;
-          Sx[bi][rr][ii] = v;
+          const int row = 4 * (lane >> 4) + ii;
+          const bool out = row < lo[bi] || row > hi[bi];
+#pragma unroll
+          for (int rr = 0; rr < RPW; ++rr) Sx[bi][rr][ii] = out ? -INFINITY : Sx[bi][rr][ii];
         }
+    }
     PFrags<NB, RPW> pf;
     paged_softmax(st, Sx, pf, lane);
     const unsigned char* vt = KCONV ? tile_v : stg + TW * RB;
-    if (!full && any_not_finite<KV8, TW * RB>(stg + TW * RB, lane)) {
-      pv_per_query<RPW, NB, HDIM, KV8 && !KCONV, RB>(st, pf, vt, a.C, a.Gp, rt0, lane, [&](int bi, int j, int c) {
-        return there[bi] && seen_from(t0[bi] + 4 * (lane >> 4) + j, Lv - a.C + c);
-      });
-    } else {
-      if constexpr (KV8 && !KCONV)
-        pv_tile_e4m3<RPW, NB, HDIM, RB>(st, pf, vt, lane);
-      else
-        pv_tile<RPW, NB, HDIM>(st, pf, vt, lane);
-    }
+    if constexpr (KV8 && !KCONV)
+      pv_tile_e4m3<RPW, NB, HDIM, RB>(st, pf, vt, lane);
+    else
+      pv_tile<RPW, NB, HDIM>(st, pf, vt, lane);
     if constexpr (NWV == 1) {
       __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the stage has been read
       asm volatile("" ::: "memory");
@@ -478,6 +527,51 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
       __syncthreads();
       if (KCONV) __syncthreads();
     }
+
+  // the tiles left out, at most two each of windows' starts and of the chunk's
+  // tokens, through stage 0 of their group's ring
+  for (int T = a0; T <= max(a1, e1); ++T) {
+    if (T > a1 && T < e0) T = e0;
+    if (T < a0 || !is_apart(T)) continue;
+    if constexpr (NWV > 1) __syncthreads();  // the ring's last stage has been read
+    const int i = T / TGW;
+    const bool mine = T % TGW == tg;
+    Block k[NB];
+    const unsigned char* stg = ring_p;
+    if (mine) {
+      fill_ids(i);
+#pragma unroll
+      for (int bi = 0; bi < NB; ++bi) k[bi] = block_at(i, bi, false);
+      issue_as(i, 0, k);
+      wait_ring<2 * LPM>(0);
+      asm volatile("" ::: "memory");
+    }
+    if constexpr (NWV > 1) __syncthreads();
+    if constexpr (KCONV)  // (a group that has no tile converts what its ring holds)
+      convert(stg);
+    if (!mine) continue;
+    f32x4 Sx[NB][RPW];
+    logits(stg, Sx);
+    auto seen = [&](int bi, int j, int pos) {
+      const int t = k[bi].t0 + 4 * (lane >> 4) + j;
+      return !k[bi].zero && t <= pos && (a.window == 0 || t > pos - a.window || t < a.first);
+    };
+#pragma unroll
+    for (int rr = 0; rr < RPW; ++rr) {
+      const int pos = Lv - a.C + min((16 * (rt0 + rr) + (lane & 15)) / a.Gp, a.C - 1);
+#pragma unroll
+      for (int bi = 0; bi < NB; ++bi)
+#pragma unroll
+        for (int ii = 0; ii < 4; ++ii) Sx[bi][rr][ii] = seen(bi, ii, pos) ? Sx[bi][rr][ii] * c2 : -INFINITY;
+    }
+    PFrags<NB, RPW> pf;
+    paged_softmax(st, Sx, pf, lane);
+    const bool apart = any_not_finite<KV8, TW * RB>(stg + TW * RB, lane);
+    pv_apart<RPW, NB, HDIM, KV8 && !KCONV, RB>(st, pf, KCONV ? tile_v : stg + TW * RB, apart, a.C, a.Gp, rt0, lane,
+                                              [&](int bi, int j, int c) { return seen(bi, j, Lv - a.C + c); });
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the stage has been read
+    asm volatile("" ::: "memory");
+  }
 
   // the groups' rows against their common maximum, summed; with one split the
   // sink's logit takes part and the output is written
