@@ -43,11 +43,11 @@ __device__ inline bool is_page(int id, int n_pages) { return (uint32_t)id < (uin
 //
 // What a query does not see must not reach it, and 0 x NaN is NaN: rows that no
 // query sees are never loaded (they repeat a visible row of their block, or are
-// zero rows), and the few tiles of which the queries see different rows (the
-// last tokens of a chunk, the starts of its windows) are left to a second loop.
-// In the loop itself all rows of a tile are seen by every query or by none;
-// with both products in one loop the compiler kept O twice (154 registers a
-// lane for one row tile of head dim 128).
+// zero rows), and a tile of which the queries see different rows (the last
+// tokens of a chunk, the starts of its windows) whose V is not finite is
+// emptied and left to a second loop, which takes the queries one by one.  (With
+// both products in one loop the compiler kept O twice, 154 registers a lane
+// for one row tile of head dim 128 instead of 120.)
 
 // What stands in for rows that are not loaded.
 __device__ const uint4 zero_row[32] = {};
@@ -212,14 +212,14 @@ __device__ inline uint4 v_operand(const unsigned char* v, int i, int nb, int lan
   }
 }
 
-// O += P V of a tile of which the queries see different rows.  Where some V is
-// not finite (apart), a product with a probability of 0 would carry a NaN into
-// the rows of the queries that do not see it: then one pass per query, with the
-// rows that it does not see taken as 0, kept in that query's rows only.
+// O += P V of a tile of which the queries see different rows and some V is not
+// finite: a product with a probability of 0 would carry a NaN into the rows of
+// the queries that do not see it.  One pass per query, with the rows that it
+// does not see taken as 0, kept in that query's rows only.
 // seen(bi, j, c): whether query c sees the lane's token j of block bi.
 template <int RPW, int NB, int HDIM, bool KV8, int RB, class Seen>
-__device__ inline void pv_apart(WaveState<RPW, HDIM>& st, const PFrags<NB, RPW>& pf, const unsigned char* v, bool apart,
-                                int C, int Gp, int rt0, int lane, Seen&& seen) {
+__device__ inline void pv_apart(WaveState<RPW, HDIM>& st, const PFrags<NB, RPW>& pf, const unsigned char* v, int C,
+                                int Gp, int rt0, int lane, Seen&& seen) {
   constexpr bool K32 = NB % 2 == 0;
   int c = 0;
   do {
@@ -228,14 +228,14 @@ __device__ inline void pv_apart(WaveState<RPW, HDIM>& st, const PFrags<NB, RPW>&
     for (int rr = 0; rr < RPW; ++rr)
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        mine[rr][k] = !apart || (16 * (rt0 + rr) + 4 * (lane >> 4) + k) / Gp == c ? 0xFFFFFFFFu : 0u;
+        mine[rr][k] = (16 * (rt0 + rr) + 4 * (lane >> 4) + k) / Gp == c ? 0xFFFFFFFFu : 0u;
 #pragma unroll
     for (int i = 0; i < (K32 ? NB / 2 : NB); ++i) {
       uint32_t keep[4];  // of the lane's tokens, two a word, in the operand's order
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int bi = K32 ? 2 * i + (j >> 1) : i, t = 2 * (j & 1);
-        keep[j] = (!apart || seen(bi, t, c) ? 0xFFFFu : 0u) | (!apart || seen(bi, t + 1, c) ? 0xFFFF0000u : 0u);
+        keep[j] = (seen(bi, t, c) ? 0xFFFFu : 0u) | (seen(bi, t + 1, c) ? 0xFFFF0000u : 0u);
       }
 #pragma unroll
       for (int nb = 0; nb < HDIM / 16; ++nb) {
@@ -258,7 +258,7 @@ __device__ inline void pv_apart(WaveState<RPW, HDIM>& st, const PFrags<NB, RPW>&
         __builtin_amdgcn_sched_barrier(0);  // one operand at a time: a rare loop is not to cost the other registers
       }
     }
-  } while (apart && ++c < C);
+  } while (++c < C);
 }
 
 // Shapes: LDS of a workgroup and what follows from the template's numbers.
@@ -269,13 +269,17 @@ struct PagedShape {
   static constexpr int RB = KV8 ? HDIM : 2 * HDIM;       // bytes of a staged cache row
   static constexpr int SB = 2 * TW * RB;                 // stage: K rows, then V rows
   static constexpr int LPM = TW * RB / 1024 / NWV;       // 1 KB loads per matrix per stage per wave
-  static constexpr int GB = fa_ring_group_bytes(NWV, TW, NS, KV8, HDIM);
-  static constexpr int IDS = 128;                        // page ids per wave, two halves
+  // E4M3 tiles of more than two waves are converted once into shared bf16 tiles;
+  // two waves convert in registers, each for itself (4 x 128K tokens, 64 rows: 129
+  // us, with shared tiles 142)
+  static constexpr bool KCONV = KV8 && NWV > 2;
+  static constexpr int GB = NS * SB + (KCONV ? 2 * TW * 2 * HDIM : 0);
+  static constexpr int IDS = NW > 4 ? 64 : 128;          // blocks described per wave, two halves
   // columns per exchange of the groups' outputs
   static constexpr int CW = TGW * ROWS * (HDIM + 4) * 4 <= (TGW * GB > 70000 ? TGW * GB : 70000) ? HDIM : HDIM / 2;
   static constexpr int EXCH = TGW * ROWS * (CW + 4) * 4;
   static constexpr int RING = TGW * GB > EXCH ? TGW * GB : EXCH;
-  static constexpr int LDS = RING + NW * IDS * 4;
+  static constexpr int LDS = RING + NW * IDS * 16;
   // workgroups per compute unit: each with its statistics and 1 KB to spare in 160 KB
   static constexpr int WGS = 160 * 1024 / (LDS + TGW * ROWS * 8 + 1024);
   static_assert(LPM >= 1 && TW * RB == 1024 * LPM * NWV && TW <= 32, "whole 1 KB loads for every wave and stage, two blocks");
@@ -305,7 +309,7 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
   using P = PagedShape<RPW, NWV, TGW, TW, NS, KV8, HDIM>;
   constexpr int NB = TW / 16, NKK = HDIM / 32, RB = P::RB, SB = P::SB, LPM = P::LPM, CPR = RB / 16, RPL = 1024 / RB;
   constexpr int SRB = 2 * HDIM, NTH = 64 * P::NW, ROWS = P::ROWS, IDS = P::IDS;
-  constexpr bool KCONV = KV8 && NWV > 1;  // K and V converted once into shared bf16 tiles
+  constexpr bool KCONV = P::KCONV;
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ float s_m[TGW][ROWS], s_l[TGW][ROWS];
 
@@ -352,24 +356,11 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
   const uint32_t ring = lds_addr(ring_p);
   unsigned char* tile_k = ring_p + NS * SB;   // KCONV: the converted tiles
   unsigned char* tile_v = tile_k + TW * SRB;
-  int32_t* ids = (int32_t*)(smem + P::RING) + wid * IDS;
+  uint4* blocks = (uint4*)(smem + P::RING) + wid * IDS;
 
-  // page of the lane's block among the next 64 of this token group
-  auto fill_ids = [&](int tile) __attribute__((always_inline)) {
-    const int e = tile * NB + lane;                          // block of the group
-    const int i = ((e / NB) * TGW + tg) * NB + e % NB;       // block of the split
-    int id = -1;
-    if (i < n_blocks) {
-      id = a.p.table[(int64_t)b * a.p.max_pages + ((token_block(span, i0 + i) * 16) >> a.p.page_shift)];
-      if (!is_page(id, a.p.n_pages)) id = -1;
-    }
-    ids[e % IDS] = id;
-    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
-    asm volatile("" ::: "memory");
-  };
-  // Tiles of which the queries see different rows: those with the starts of the
-  // later queries' windows (or where first tokens end and a window begins in
-  // one block) and those with the chunk's own tokens.
+  // Tiles apart, of which the queries see different rows: those with the starts
+  // of the later queries' windows (or where first tokens end and a window begins
+  // in one block) and those with the chunk's own tokens; at most two of each.
   int a0 = 0, a1 = -1, e0 = 0, e1 = -1;
   {
     const bool gap = a.window > 0 && (a.first + 15) / 16 > span.w0 && a.first < span.lo;
@@ -385,22 +376,39 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
     }
   }
   auto is_apart = [&](int T) { return (T >= a0 && T <= a1) || (T >= e0 && T <= e1); };
-
-  // A block's page and first token; the rows [lo, hi] of it are seen by some
-  // query (rows outside repeat one of them).  zero: of no row.
-  struct Block {
-    int id, t0, lo, hi;
-    bool zero;
+  auto round_apart = [&](int i) {  // a tile apart among the groups' tiles i
+    const int T0 = i * TGW, T1 = T0 + TGW - 1;
+    return (a0 <= min(a1, T1) && a1 >= T0) || (e0 <= min(e1, T1) && e1 >= T0);
   };
-  auto block_at = [&](int tile, int bi, bool apart) __attribute__((always_inline)) {
-    Block k;
-    k.id = __builtin_amdgcn_readfirstlane(ids[(tile * NB + bi) % IDS]);
-    const int i = i0 + (tile * TGW + tg) * NB + bi;
-    k.t0 = 16 * token_block(span, i);
-    k.zero = k.id < 0 || apart;
-    k.lo = k.t0 < a.first ? 0 : max(0, span.lo - k.t0);
-    k.hi = min(15, (i < span.nf ? min(a.first, Lv) : Lv) - 1 - k.t0);
-    return k;
+  // whether the query at pos sees the token
+  auto sees = [&](int pos, int t) { return t <= pos && (a.window == 0 || t > pos - a.window || t < a.first); };
+  bool deferred = false;
+
+  // Blocks are described 64 at a time, a lane each, in LDS: x, y: byte offset of
+  // the first row in the pool; z: the rows [lo, hi] that some query sees, lo +
+  // 256 hi (rows outside repeat one of them), or NONE (zero rows: no page); w:
+  // first token.  The loop over tiles then needs a few scalars a block.
+  constexpr uint32_t ALL = 15u << 8, NONE = 16u;
+  auto describe = [&](int tile) __attribute__((always_inline)) {
+    const int e = tile * NB + lane;                     // block of the group
+    const int T = (e / NB) * TGW + tg, i = T * NB + e % NB;  // tile and block of the split
+    uint4 d = make_uint4(0, 0, NONE, 0);
+    if (i < n_blocks) {
+      const int v = i0 + i, t0 = 16 * token_block(span, v);
+      const int id = a.p.table[(int64_t)b * a.p.max_pages + (t0 >> a.p.page_shift)];
+      if (is_page(id, a.p.n_pages)) {
+        const int64_t off = id * a.p.stride_p + (t0 & (a.p.page - 1)) * a.p.stride_t;
+        const int lo = t0 < a.first ? 0 : max(0, span.lo - t0);
+        const int hi = min(15, (v < span.nf ? min(a.first, Lv) : Lv) - 1 - t0);
+        d = make_uint4((uint32_t)off, (uint32_t)(off >> 32), (uint32_t)(lo | hi << 8), (uint32_t)t0);
+      }
+    }
+    if (IDS == 128 || lane < IDS / 2) blocks[e % IDS] = d;
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+  };
+  auto rows_of = [&](int tile, int bi) __attribute__((always_inline)) {
+    return (uint32_t)__builtin_amdgcn_readfirstlane(blocks[(tile * NB + bi) % IDS].z);
   };
   const int lrow = lane / CPR;  // this lane's row of a 1 KB load
   auto lane_offset = [&](int row, int from) __attribute__((always_inline)) {
@@ -414,16 +422,20 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
     lane_off[u] = lane_offset(row, row & 15);
   }
   // (every stage issues all its loads: the waits count them)
-  auto issue_as = [&](int tile, int stage, const Block (&k)[NB]) __attribute__((always_inline)) {
+  auto issue_to = [&](int tile, int stage) __attribute__((always_inline)) {
     const uint32_t base = ring + (uint32_t)(stage * SB);
     const unsigned char *kp[NB], *vp[NB];
+    uint32_t z[NB];
     bool all = true;
 #pragma unroll
     for (int bi = 0; bi < NB; ++bi) {
-      const int64_t off = k[bi].id * a.p.stride_p + (k[bi].t0 & (a.p.page - 1)) * a.p.stride_t;
-      kp[bi] = k[bi].zero ? (const unsigned char*)zero_row : Kg + off;
-      vp[bi] = k[bi].zero ? (const unsigned char*)zero_row : Vg + off;
-      all &= !k[bi].zero && k[bi].lo == 0 && k[bi].hi == 15;
+      const uint4 d = blocks[(tile * NB + bi) % IDS];
+      z[bi] = (uint32_t)__builtin_amdgcn_readfirstlane(d.z);
+      const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(d.x) |
+                           (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(d.y) << 32;
+      kp[bi] = z[bi] == NONE ? (const unsigned char*)zero_row : Kg + off;
+      vp[bi] = z[bi] == NONE ? (const unsigned char*)zero_row : Vg + off;
+      all &= z[bi] == ALL;
     }
 #pragma unroll
     for (int u = 0; u < LPM; ++u) {
@@ -432,19 +444,16 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
       uint32_t lo = lane_off[u];
       if (!all) {
         const int row = RPL * n + lrow;
-        const int from = max(second ? k[NB - 1].lo : k[0].lo, min(row & 15, second ? k[NB - 1].hi : k[0].hi));
-        lo = lane_offset(row, (second ? k[NB - 1].zero : k[0].zero) ? 0 : from);
+        const uint32_t r = second ? z[NB - 1] : z[0];
+        lo = lane_offset(row, r == NONE ? 0 : max((int)(r & 255u), min(row & 15, (int)(r >> 8))));
       }
       dma16_s<NTL>(second ? kp[NB - 1] : kp[0], lo, __builtin_amdgcn_readfirstlane(base + 1024 * n));
       dma16_s<NTL>(second ? vp[NB - 1] : vp[0], lo, __builtin_amdgcn_readfirstlane(base + TW * RB + 1024 * n));
     }
   };
   auto issue = [&](int tile) __attribute__((always_inline)) {
-    if (tile % (IDS / 2 / NB) == 0) fill_ids(tile);
-    Block k[NB];
-#pragma unroll
-    for (int bi = 0; bi < NB; ++bi) k[bi] = block_at(tile, bi, is_apart(tile * TGW + tg));
-    issue_as(tile, tile % NS, k);
+    if (tile % (IDS / 2 / NB) == 0) describe(tile);
+    issue_to(tile, tile % NS);
   };
   auto logits = [&](const unsigned char* stg, f32x4 (&Sx)[NB][RPW]) __attribute__((always_inline)) {
 #pragma unroll
@@ -485,29 +494,52 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
     convert(stg);
     f32x4 Sx[NB][RPW];
     logits(stg, Sx);
-    int lo[NB], hi[NB];  // rows that the queries see
+    uint32_t z[NB];  // rows that the queries see
     bool full = true;
 #pragma unroll
     for (int bi = 0; bi < NB; ++bi) {
-      const Block k = block_at(i, bi, is_apart(i * TGW + tg));
-      lo[bi] = k.lo;
-      hi[bi] = k.zero ? -1 : k.hi;
-      full &= lo[bi] == 0 && hi[bi] == 15;
+      z[bi] = rows_of(i, bi);
+      full &= z[bi] == ALL;
     }
 #pragma unroll
     for (int bi = 0; bi < NB; ++bi)
 #pragma unroll
       for (int rr = 0; rr < RPW; ++rr) Sx[bi][rr] *= c2;
-    if (!full) {
+    const bool apart = is_apart(i * TGW + tg);
+    if (!full || apart) {
 #pragma unroll
       for (int bi = 0; bi < NB; ++bi)
 #pragma unroll
         for (int ii = 0; ii < 4; ++ii) {
           const int row = 4 * (lane >> 4) + ii;
-          const bool out = row < lo[bi] || row > hi[bi];
+          const bool out = row < (int)(z[bi] & 255u) || row > (int)(z[bi] >> 8);
 #pragma unroll
           for (int rr = 0; rr < RPW; ++rr) Sx[bi][rr][ii] = out ? -INFINITY : Sx[bi][rr][ii];
         }
+    }
+    if (NWV == 1 ? apart : round_apart(i)) {
+      unsigned char* v = ring_p + (i % NS) * SB + TW * RB;
+      const bool bad = apart && any_not_finite<KV8, TW * RB>(v, lane);
+      if constexpr (NWV > 1) __syncthreads();  // every wave of the group has looked
+      if (apart) {
+#pragma unroll
+        for (int bi = 0; bi < NB; ++bi) {
+          const int t0 = __builtin_amdgcn_readfirstlane(blocks[(i * NB + bi) % IDS].w) + 4 * (lane >> 4);
+#pragma unroll
+          for (int rr = 0; rr < RPW; ++rr) {
+            const int pos = Lv - a.C + min((16 * (rt0 + rr) + (lane & 15)) / a.Gp, a.C - 1);
+#pragma unroll
+            for (int ii = 0; ii < 4; ++ii) Sx[bi][rr][ii] = !bad && sees(pos, t0 + ii) ? Sx[bi][rr][ii] : -INFINITY;
+          }
+        }
+        if (bad) {  // empty: probabilities and V are 0
+          deferred = true;
+          unsigned char* x = KCONV ? tile_v : v;
+#pragma unroll
+          for (int k = 0; k < TW * (KCONV ? SRB : RB) / 1024; ++k) *(uint4*)(x + 1024 * k + 16 * lane) = make_uint4(0, 0, 0, 0);
+          asm volatile("" ::: "memory");
+        }
+      }
     }
     PFrags<NB, RPW> pf;
     paged_softmax(st, Sx, pf, lane);
@@ -526,52 +558,56 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
     for (int i = ntiles; i < (all_tiles + TGW - 1) / TGW; ++i) {
       __syncthreads();
       if (KCONV) __syncthreads();
+      if (round_apart(i)) __syncthreads();
     }
 
-  // the tiles left out, at most two each of windows' starts and of the chunk's
-  // tokens, through stage 0 of their group's ring
-  for (int T = a0; T <= max(a1, e1); ++T) {
-    if (T > a1 && T < e0) T = e0;
-    if (T < a0 || !is_apart(T)) continue;
-    if constexpr (NWV > 1) __syncthreads();  // the ring's last stage has been read
-    const int i = T / TGW;
-    const bool mine = T % TGW == tg;
-    Block k[NB];
-    const unsigned char* stg = ring_p;
-    if (mine) {
-      fill_ids(i);
+  // the tiles left out, through stage 0 of their group's ring
+  if constexpr (NWV > 1) {
+    if (a1 >= a0 || e1 >= e0) deferred = __syncthreads_or(deferred);
+  }
+  if (deferred)
+    for (int T = a0; T <= max(a1, e1); ++T) {
+      if (T > a1 && T < e0) T = e0;
+      if (!is_apart(T)) continue;
+      if constexpr (NWV > 1) __syncthreads();  // the ring's last stage has been read
+      const int i = T / TGW;
+      const bool mine = T % TGW == tg;
+      const unsigned char* stg = ring_p;
+      if (mine) {
+        describe(i);
+        issue_to(i, 0);
+        wait_ring<2 * LPM>(0);
+        asm volatile("" ::: "memory");
+      }
+      if constexpr (NWV > 1) __syncthreads();
+      convert(stg);  // (KCONV: a group that has no tile converts what its ring holds)
+      if (!mine || !any_not_finite<KV8, TW * RB>(stg + TW * RB, lane)) continue;
+      f32x4 Sx[NB][RPW];
+      logits(stg, Sx);
+      int t0[NB];
+      bool there[NB];
 #pragma unroll
-      for (int bi = 0; bi < NB; ++bi) k[bi] = block_at(i, bi, false);
-      issue_as(i, 0, k);
-      wait_ring<2 * LPM>(0);
+      for (int bi = 0; bi < NB; ++bi) {
+        t0[bi] = __builtin_amdgcn_readfirstlane(blocks[(i * NB + bi) % IDS].w) + 4 * (lane >> 4);
+        there[bi] = rows_of(i, bi) != NONE;
+      }
+#pragma unroll
+      for (int rr = 0; rr < RPW; ++rr) {
+        const int pos = Lv - a.C + min((16 * (rt0 + rr) + (lane & 15)) / a.Gp, a.C - 1);
+#pragma unroll
+        for (int bi = 0; bi < NB; ++bi)
+#pragma unroll
+          for (int ii = 0; ii < 4; ++ii)
+            Sx[bi][rr][ii] = there[bi] && sees(pos, t0[bi] + ii) ? Sx[bi][rr][ii] * c2 : -INFINITY;
+      }
+      PFrags<NB, RPW> pf;
+      paged_softmax(st, Sx, pf, lane);
+      pv_apart<RPW, NB, HDIM, KV8 && !KCONV, RB>(
+          st, pf, KCONV ? tile_v : stg + TW * RB, a.C, a.Gp, rt0, lane,
+          [&](int bi, int j, int c) { return there[bi] && sees(Lv - a.C + c, t0[bi] + j); });
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the stage has been read
       asm volatile("" ::: "memory");
     }
-    if constexpr (NWV > 1) __syncthreads();
-    if constexpr (KCONV)  // (a group that has no tile converts what its ring holds)
-      convert(stg);
-    if (!mine) continue;
-    f32x4 Sx[NB][RPW];
-    logits(stg, Sx);
-    auto seen = [&](int bi, int j, int pos) {
-      const int t = k[bi].t0 + 4 * (lane >> 4) + j;
-      return !k[bi].zero && t <= pos && (a.window == 0 || t > pos - a.window || t < a.first);
-    };
-#pragma unroll
-    for (int rr = 0; rr < RPW; ++rr) {
-      const int pos = Lv - a.C + min((16 * (rt0 + rr) + (lane & 15)) / a.Gp, a.C - 1);
-#pragma unroll
-      for (int bi = 0; bi < NB; ++bi)
-#pragma unroll
-        for (int ii = 0; ii < 4; ++ii) Sx[bi][rr][ii] = seen(bi, ii, pos) ? Sx[bi][rr][ii] * c2 : -INFINITY;
-    }
-    PFrags<NB, RPW> pf;
-    paged_softmax(st, Sx, pf, lane);
-    const bool apart = any_not_finite<KV8, TW * RB>(stg + TW * RB, lane);
-    pv_apart<RPW, NB, HDIM, KV8 && !KCONV, RB>(st, pf, KCONV ? tile_v : stg + TW * RB, apart, a.C, a.Gp, rt0, lane,
-                                              [&](int bi, int j, int c) { return seen(bi, j, Lv - a.C + c); });
-    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the stage has been read
-    asm volatile("" ::: "memory");
-  }
 
   // the groups' rows against their common maximum, summed; with one split the
   // sink's logit takes part and the output is written
@@ -1120,11 +1156,11 @@ __global__ __launch_bounds__(NTP) void k_pages_copy(PagesCopyArgs a) {
   X(1, false, 128, 1, 1, 4, 16, 2) X(2, false, 128, 2, 1, 4, 16, 2)    \
   X(4, false, 128, 2, 2, 2, 32, 2) X(8, false, 128, 2, 4, 1, 32, 2)    \
   X(1, false, 256, 1, 1, 4, 16, 2) X(2, false, 256, 1, 2, 2, 16, 2)    \
-  X(4, false, 256, 1, 4, 1, 32, 2) X(8, false, 256, 1, 8, 1, 32, 2)    \
+  X(4, false, 256, 1, 4, 1, 32, 3) X(8, false, 256, 1, 8, 1, 32, 3)    \
   X(1, true, 128, 1, 1, 4, 32, 2) X(2, true, 128, 2, 1, 4, 32, 2)      \
   X(4, true, 128, 2, 2, 2, 32, 2) X(8, true, 128, 2, 4, 1, 32, 2)      \
   X(1, true, 256, 1, 1, 4, 16, 2) X(2, true, 256, 1, 2, 2, 16, 2)      \
-  X(4, true, 256, 1, 4, 1, 32, 2) X(8, true, 256, 1, 8, 1, 32, 2)
+  X(4, true, 256, 1, 4, 1, 32, 2) X(8, true, 256, 1, 8, 1, 32, 4)
 #endif
 
 PagedAttnShape paged_attn_shape(int RT, bool kv8, int hd) {
