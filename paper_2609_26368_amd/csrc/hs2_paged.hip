@@ -9,6 +9,8 @@
 //   k_pages_reorder  rows take over their parents' entries
 //   k_pages_list, k_pages_compact   moves that pack the pool; table and counts after them
 //   k_pages_copy     the moves' contents
+#include <cfloat>
+
 #include "hs2_device.h"
 #include "hs2_launch.h"
 
@@ -137,45 +139,68 @@ __device__ inline bool paged_locate(const PagedAttnArgs& a, int n0, int S, int i
   return false;
 }
 
-// Running softmax with BPW blocks of logits (log2 units, -inf: not seen);
-// returns the probabilities as A operands of P V.  They are rounded to bf16,
-// the cache's type (half a step, 2^-8), and the normaliser sums the rounded
-// values, so that the weights still sum to one.  m is raised only past
-// LAZY_MARGIN.
+// A wave's running state: the reference maximum and O as in WaveState, and the
+// normalisers as a column of O would be, the product of the probabilities with
+// ones: they sum the rounded probabilities (so that the weights sum to one)
+// without vector instructions, in the row layout of O.
+template <int RPW, int HDIM>
+struct PagedState : WaveState<RPW, HDIM> {
+  f32x4 z[RPW];
+  __device__ inline void init() {
+    WaveState<RPW, HDIM>::init();
+#pragma unroll
+    for (int r = 0; r < RPW; ++r) z[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+};
+
+// Running softmax with BPW blocks of products q k (-inf: not seen), c2 > 0
+// times which are the logits in log2 units; returns the probabilities as A
+// operands of P V, rounded to bf16, the cache's type (half a step, 2^-8).  m is
+// raised only past LAZY_MARGIN.
 template <int RPW, int BPW, int HDIM>
-__device__ inline void paged_softmax(WaveState<RPW, HDIM>& st, f32x4 (&S)[BPW][RPW], PFrags<BPW, RPW>& pf, int lane) {
+__device__ inline void paged_softmax(PagedState<RPW, HDIM>& st, const f32x4 (&S)[BPW][RPW], float c2,
+                                     PFrags<BPW, RPW>& pf, int lane) {
 #pragma unroll
   for (int rr = 0; rr < RPW; ++rr) {
     float mx = -INFINITY;
 #pragma unroll
     for (int bi = 0; bi < BPW; ++bi)
       mx = fmaxf(mx, fmaxf(fmaxf(S[bi][rr][0], S[bi][rr][1]), fmaxf(S[bi][rr][2], S[bi][rr][3])));
-    mx = max_xor32(max_xor16(mx));
+    mx = max_xor32(max_xor16(mx)) * c2;
     if (__ballot(mx > st.m[rr] + LAZY_MARGIN)) {
       const float mnew = fmaxf(st.m[rr], mx);
       const float alpha = mnew == -INFINITY ? 1.f : fast_exp2(st.m[rr] - mnew);  // m = -inf -> 0
       st.m[rr] = mnew;
-      st.l[rr] *= alpha;
       float a4[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) a4[i] = __shfl(alpha, 4 * (lane >> 4) + i);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st.z[rr][i] *= a4[i];
 #pragma unroll
       for (int nb = 0; nb < WaveState<RPW, HDIM>::NBC; ++nb)
 #pragma unroll
         for (int i = 0; i < 4; ++i) st.o[rr][nb][i] *= a4[i];
     }
     const float msub = st.m[rr] == -INFINITY ? 0.f : st.m[rr];
-    float psum = 0.f;
 #pragma unroll
     for (int bi = 0; bi < BPW; ++bi) {
-      const uint32_t lo = pack_bf16x2(fast_exp2(S[bi][rr][0] - msub), fast_exp2(S[bi][rr][1] - msub));
-      const uint32_t hi = pack_bf16x2(fast_exp2(S[bi][rr][2] - msub), fast_exp2(S[bi][rr][3] - msub));
-      psum += (__uint_as_float(lo << 16) + __uint_as_float(lo & 0xFFFF0000u)) +
-              (__uint_as_float(hi << 16) + __uint_as_float(hi & 0xFFFF0000u));
-      pf.set(bi, rr, lo, hi);
+      float p[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = fast_exp2(__builtin_fmaf(S[bi][rr][i], c2, -msub));
+      pf.set(bi, rr, pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]));
     }
-    st.l[rr] += psum;
   }
+  constexpr uint32_t ONES = 0x3F803F80u;
+  constexpr bool K32 = BPW % 2 == 0;
+#pragma unroll
+  for (int i = 0; i < (K32 ? BPW / 2 : BPW); ++i)
+#pragma unroll
+    for (int rr = 0; rr < RPW; ++rr) {
+      if constexpr (K32)
+        st.z[rr] = mfma_k32(pf.w[i][rr], make_uint4(ONES, ONES, ONES, ONES), st.z[rr]);
+      else
+        st.z[rr] = mfma_k16(pf.h[i][rr], make_uint2(ONES, ONES), st.z[rr]);
+    }
 }
 
 // Whether a staged tile of bytes holds an infinity or NaN (bf16: exponent of
@@ -218,7 +243,7 @@ __device__ inline uint4 v_operand(const unsigned char* v, int i, int nb, int lan
 // does not see taken as 0, kept in that query's rows only.
 // seen(bi, j, c): whether query c sees the lane's token j of block bi.
 template <int RPW, int NB, int HDIM, bool KV8, int RB, class Seen>
-__device__ inline void pv_apart(WaveState<RPW, HDIM>& st, const PFrags<NB, RPW>& pf, const unsigned char* v, int C,
+__device__ inline void pv_apart(PagedState<RPW, HDIM>& st, const PFrags<NB, RPW>& pf, const unsigned char* v, int C,
                                 int Gp, int rt0, int lane, Seen&& seen) {
   constexpr bool K32 = NB % 2 == 0;
   int c = 0;
@@ -282,6 +307,7 @@ struct PagedShape {
   static constexpr int LDS = RING + NW * IDS * 16;
   // workgroups per compute unit: each with its statistics and 1 KB to spare in 160 KB
   static constexpr int WGS = 160 * 1024 / (LDS + TGW * ROWS * 8 + 1024);
+  static_assert(WGS >= 1, "fits a compute unit");
   static_assert(LPM >= 1 && TW * RB == 1024 * LPM * NWV && TW <= 32, "whole 1 KB loads for every wave and stage, two blocks");
 };
 
@@ -349,7 +375,8 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
       if (!real) q[rr][kk] = make_uint4(0, 0, 0, 0);
     }
   }
-  const float c2 = KV8 ? a.c2 * a.k_scale[g] : a.c2;
+  float c2 = KV8 ? a.c2 * a.k_scale[g] : a.c2;
+  if (c2 < FLT_MIN) c2 = FLT_MIN;  // -inf times it stays -inf
   const unsigned char* Kg = a.p.K + g * a.p.stride_h;
   const unsigned char* Vg = a.p.V + g * a.p.stride_h;
   unsigned char* ring_p = smem + tg * P::GB;
@@ -474,7 +501,7 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
     }
   };
 
-  WaveState<RPW, HDIM> st;
+  PagedState<RPW, HDIM> st;
   st.init();
   // a group of one wave refills a stage as soon as it has read it; the waves
   // of a shared ring meet once a stage, which leaves NS - 1 stages in flight
@@ -501,10 +528,6 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
       z[bi] = rows_of(i, bi);
       full &= z[bi] == ALL;
     }
-#pragma unroll
-    for (int bi = 0; bi < NB; ++bi)
-#pragma unroll
-      for (int rr = 0; rr < RPW; ++rr) Sx[bi][rr] *= c2;
     const bool apart = is_apart(i * TGW + tg);
     if (!full || apart) {
 #pragma unroll
@@ -542,7 +565,7 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
       }
     }
     PFrags<NB, RPW> pf;
-    paged_softmax(st, Sx, pf, lane);
+    paged_softmax(st, Sx, c2, pf, lane);
     const unsigned char* vt = KCONV ? tile_v : stg + TW * RB;
     if constexpr (KV8 && !KCONV)
       pv_tile_e4m3<RPW, NB, HDIM, RB>(st, pf, vt, lane);
@@ -598,10 +621,10 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
         for (int bi = 0; bi < NB; ++bi)
 #pragma unroll
           for (int ii = 0; ii < 4; ++ii)
-            Sx[bi][rr][ii] = there[bi] && sees(pos, t0[bi] + ii) ? Sx[bi][rr][ii] * c2 : -INFINITY;
+            Sx[bi][rr][ii] = there[bi] && sees(pos, t0[bi] + ii) ? Sx[bi][rr][ii] : -INFINITY;
       }
       PFrags<NB, RPW> pf;
-      paged_softmax(st, Sx, pf, lane);
+      paged_softmax(st, Sx, c2, pf, lane);
       pv_apart<RPW, NB, HDIM, KV8 && !KCONV, RB>(
           st, pf, KCONV ? tile_v : stg + TW * RB, a.C, a.Gp, rt0, lane,
           [&](int bi, int j, int c) { return there[bi] && sees(Lv - a.C + c, t0[bi] + j); });
@@ -614,11 +637,10 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
   const bool whole = n_splits == 1;
 #pragma unroll
   for (int rr = 0; rr < RPW; ++rr) {
-    const float l = sum_xor32(sum_xor16(st.l[rr]));
-    if (lane < 16) {
-      s_m[tg][16 * (rt0 + rr) + lane] = st.m[rr];
-      s_l[tg][16 * (rt0 + rr) + lane] = l;
-    }
+    if (lane < 16) s_m[tg][16 * (rt0 + rr) + lane] = st.m[rr];
+    if ((lane & 15) == 0)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s_l[tg][16 * (rt0 + rr) + 4 * (lane >> 4) + i] = st.z[rr][i];
   }
   const float v_scale = KV8 ? a.v_scale[g] : 1.f;
   __syncthreads();  // and every ring is free
@@ -1155,11 +1177,11 @@ __global__ __launch_bounds__(NTP) void k_pages_copy(PagesCopyArgs a) {
 #define HS2_PAGED_SHAPES(X)                                            \
   X(1, false, 128, 1, 1, 4, 16, 2) X(2, false, 128, 2, 1, 4, 16, 2)    \
   X(4, false, 128, 2, 2, 2, 32, 2) X(8, false, 128, 2, 4, 1, 32, 2)    \
-  X(1, false, 256, 1, 1, 4, 16, 2) X(2, false, 256, 1, 2, 2, 16, 2)    \
-  X(4, false, 256, 1, 4, 1, 32, 3) X(8, false, 256, 1, 8, 1, 32, 3)    \
+  X(1, false, 256, 1, 1, 4, 16, 2) X(2, false, 256, 1, 2, 2, 32, 2)    \
+  X(4, false, 256, 1, 4, 1, 32, 3) X(8, false, 256, 1, 8, 1, 32, 4)    \
   X(1, true, 128, 1, 1, 4, 32, 2) X(2, true, 128, 2, 1, 4, 32, 2)      \
   X(4, true, 128, 2, 2, 2, 32, 2) X(8, true, 128, 2, 4, 1, 32, 2)      \
-  X(1, true, 256, 1, 1, 4, 16, 2) X(2, true, 256, 1, 2, 2, 16, 2)      \
+  X(1, true, 256, 1, 1, 4, 16, 2) X(2, true, 256, 1, 2, 2, 32, 2)      \
   X(4, true, 256, 1, 4, 1, 32, 2) X(8, true, 256, 1, 8, 1, 32, 4)
 #endif
 
