@@ -143,6 +143,7 @@ struct DeviceInfo {
   int cus = 256;
   int fa_wgs[2][4][kFaVariants] = {};  // [E4M3 cache][log2 RT][variant]; 0 = unknown
   int pool_wgs[2][2][4][7][17] = {};   // k_pool: [head dim 256][E4M3 cache][log2 RT][log2 Gp][C]; 0 = unknown
+  int paged_wgs[2][2][4] = {};         // paged attention: [head dim 256][E4M3 cache][log2 RT]; 0 = unknown
   void* scratch = nullptr;             // this device's address of `scratch` (hs2_sparse_attn_noalloc)
 };
 
@@ -452,6 +453,11 @@ hs2_status ensure_device_init(const DeviceInfo** info) {
                   hipSuccess)
                 return fail(HS2_ERR_HIP, "occupancy query: %s", hipGetErrorString(e));
       }
+    for (int h = 0; h < 2; ++h)
+      for (int f = 0; f < 2; ++f)
+        for (int l = 0; l < 4; ++l)
+          if ((e = paged_attn_wgs(1 << l, f == 1, h ? 256 : 128, &di.paged_wgs[h][f][l])) != hipSuccess)
+            return fail(HS2_ERR_HIP, "occupancy query: %s", hipGetErrorString(e));
     if ((e = hipGetSymbolAddress(&di.scratch, HIP_SYMBOL(scratch))) != hipSuccess || !di.scratch)
       return fail(HS2_ERR_HIP, "hipGetSymbolAddress(scratch): %s", hipGetErrorString(e));
     g_dev[dev] = di;
@@ -1043,7 +1049,8 @@ PagedPlan paged_plan(const hs2_paged_dims* d, bool kv8, int32_t window, int32_t 
   const PagedAttnShape sh = paged_attn_shape(p.RT, kv8, d->head_dim);
   p.rows = sh.rows;
   const int64_t units = (int64_t)d->batch * d->n_kv_heads;
-  const int64_t cus = di ? di->cus : 256, round = cus * sh.wgs;
+  const int wgs = di ? di->paged_wgs[d->head_dim == 256][kv8][ilog2(p.RT)] : 0;
+  const int64_t cus = di ? di->cus : 256, round = cus * (wgs > 0 ? wgs : sh.wgs);
   // the most blocks that a chunk can see
   int64_t cap = cdiv((int64_t)d->page * d->max_pages, 16);
   if (window > 0) cap = std::min(cap, cdiv(first, 16) + cdiv((int64_t)window + d->n_queries - 1, 16) + 1);

@@ -213,8 +213,9 @@ struct PagedAttnArgs {
   const uint16_t* gate;    // [B, C, Hq, hd] or null
 };
 struct PagedAttnShape {
-  int rows, align, wgs;  // partial rows, blocks that splits are multiples of, workgroups per compute unit
+  int rows, align, wgs;  // partial rows, blocks that splits are multiples of, workgroups per compute unit (by LDS)
 };
+hipError_t paged_attn_wgs(int RT, bool kv8, int hd, int* wgs);  // on the current device
 PagedAttnShape paged_attn_shape(int RT, bool kv8, int hd);
 hipError_t set_paged_smem_limits();
 hipError_t launch_paged_attn(const PagedAttnArgs& a, int RT, hipStream_t s);

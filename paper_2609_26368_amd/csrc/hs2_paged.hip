@@ -9,6 +9,7 @@
 //   k_pages_reorder  rows take over their parents' entries
 //   k_pages_list, k_pages_compact   moves that pack the pool; table and counts after them
 //   k_pages_copy     the moves' contents
+#include <algorithm>
 #include <cfloat>
 
 #include "hs2_device.h"
@@ -305,10 +306,9 @@ struct PagedShape {
   static constexpr int EXCH = TGW * ROWS * (CW + 4) * 4;
   static constexpr int RING = TGW * GB > EXCH ? TGW * GB : EXCH;
   static constexpr int LDS = RING + NW * IDS * 16;
-  // workgroups per compute unit: each with its statistics and 1 KB to spare in 160 KB
-  static constexpr int WGS = 160 * 1024 / (LDS + TGW * ROWS * 8 + 1024);
-  static_assert(WGS >= 1, "fits a compute unit");
+  static constexpr int LDS_ALL = LDS + TGW * ROWS * 8;   // with the row statistics
   static_assert(LPM >= 1 && TW * RB == 1024 * LPM * NWV && TW <= 32, "whole 1 KB loads for every wave and stage, two blocks");
+  static_assert(LDS_ALL <= 160 * 1024, "fits a compute unit");
 };
 
 // Weight of a part with maximum m against the common maximum M (0 where it
@@ -331,7 +331,10 @@ __device__ inline void paged_store4(float4 o, float Z, float v_scale, const uint
 }
 
 template <int RPW, int NWV, int TGW, int TW, int NS, bool KV8, int HDIM, bool NTL>
-__global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) {
+#ifndef WPE
+#define WPE 1
+#endif
+__global__ __launch_bounds__(64 * NWV * TGW, WPE) void k_paged_attn(PagedAttnArgs a) {
   using P = PagedShape<RPW, NWV, TGW, TW, NS, KV8, HDIM>;
   constexpr int NB = TW / 16, NKK = HDIM / 32, RB = P::RB, SB = P::SB, LPM = P::LPM, CPR = RB / 16, RPL = 1024 / RB;
   constexpr int SRB = 2 * HDIM, NTH = 64 * P::NW, ROWS = P::ROWS, IDS = P::IDS;
@@ -1189,11 +1192,27 @@ PagedAttnShape paged_attn_shape(int RT, bool kv8, int hd) {
 #define HS2_PAGED_SHAPE(rt, f8, hdim, rpw, nwv, tgw, tw, ns)             \
   if (RT == rt && kv8 == f8 && hd == hdim) {                             \
     using P = PagedShape<rpw, nwv, tgw, tw, ns, f8, hdim>;               \
-    return PagedAttnShape{P::ROWS, tgw * tw / 16, P::WGS};               \
+    return PagedAttnShape{P::ROWS, tgw * tw / 16, 160 * 1024 / (P::LDS_ALL + 1024)};  \
   }
   HS2_PAGED_SHAPES(HS2_PAGED_SHAPE)
 #undef HS2_PAGED_SHAPE
   return PagedAttnShape{0, 0, 0};
+}
+
+// Workgroups resident on a compute unit: the runtime's figure, each with 1 KB
+// of LDS to spare (as occupancy_capped of the full attention).
+hipError_t paged_attn_wgs(int RT, bool kv8, int hd, int* wgs) {
+#define HS2_PAGED_WGS(rt, f8, hdim, rpw, nwv, tgw, tw, ns)                                                \
+  if (RT == rt && kv8 == f8 && hd == hdim) {                                                              \
+    using P = PagedShape<rpw, nwv, tgw, tw, ns, f8, hdim>;                                                \
+    const hipError_t e = hipOccupancyMaxActiveBlocksPerMultiprocessor(                                    \
+        wgs, (const void*)k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim, true>, 64 * P::NW, P::LDS);       \
+    *wgs = std::min(*wgs, 160 * 1024 / (P::LDS_ALL + 1024));                                              \
+    return e;                                                                                             \
+  }
+  HS2_PAGED_SHAPES(HS2_PAGED_WGS)
+#undef HS2_PAGED_WGS
+  return hipErrorInvalidValue;
 }
 
 template <int LDS>
