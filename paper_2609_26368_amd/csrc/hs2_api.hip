@@ -978,8 +978,6 @@ hs2_status hs2_stream_read_probe(const void* src, size_t bytes, int32_t mode, ui
 namespace {
 
 constexpr int kMaxPages = 1 << 24;  // of a pool: their chunks' prefix sums sit in LDS
-// paged attention of at most so many 16-token blocks: one workgroup finishes a KV head
-constexpr int kPagedSingleBlocks = 64;
 
 // kv8: E4M3 strides
 hs2_status check_paged(const hs2_paged_dims* d, bool kv8) {
@@ -1054,15 +1052,29 @@ PagedPlan paged_plan(const hs2_paged_dims* d, bool kv8, int32_t window, int32_t 
   // the most blocks that a chunk can see
   int64_t cap = cdiv((int64_t)d->page * d->max_pages, 16);
   if (window > 0) cap = std::min(cap, cdiv(first, 16) + cdiv((int64_t)window + d->n_queries - 1, 16) + 1);
-  p.sp.cap_blocks = (int)cap;
-  p.sp.align = sh.align;
-  p.sp.single = cap <= kPagedSingleBlocks;
-  p.sp.fixed = p.sp.single ? (int)round_up(cap, sh.align) : 0;
-  p.sp.min_blocks = (int)round_up(16, sh.align);
-  p.sp.few_items = (int)std::min(cus, round);
-  // up to four rounds where the KV heads would not be cut evenly in one
-  const int64_t balance = std::min<int64_t>(4, std::max<int64_t>(1, cdiv(4 * units, round)));
-  p.sp.n_items = (int)std::min(std::max(round * balance, units + round / 4), units * cdiv(cap, sh.align));
+  PagedSplit& sp = p.sp;
+  sp.cap_blocks = (int)cap;
+  sp.align = sh.align;
+  sp.min_blocks = (int)round_up(16, sh.align);
+  sp.few_items = (int)std::min(cus, round);
+  sp.resident = (int)round;
+  // the grid: up to four rounds of items (paged_items), one where the KV heads are few
+  const int64_t rounds = 8 * units <= round ? 1 : 4;
+  sp.n_items = (int)std::min(std::max(rounds * round, units + round / 4), units * cdiv(cap, sh.align));
+  // (a workgroup alone against one of two a compute unit, by row tiles: measured
+  // 4, 3.4, 1.9; of one a unit at head dim 256 2.1 and, four row tiles, 1.4)
+  const float alone[4] = {4.f, 3.f, 2.f, 1.5f};
+  sp.alone = std::max(1.25f, alone[ilog2(p.RT)] * (float)round / (2.f * (float)cus));
+  sp.item = 4.f + 4.f * p.RT / (kv8 ? 1.f : 2.f);
+  sp.merge = 8.f;
+  // Without the lengths: what is short at its longest is one split; so is a
+  // window's span, which long sequences have in common, where one split is
+  // estimated to end first if all have it
+  const float capf = (float)cap;
+  sp.single = 1.25f * capf <= 12.f * sp.alone ||
+              ((float)units * sp.alone >= 1.25f * (float)sp.resident && 1.25f * capf <= 24.f * sp.alone);
+  if (window > 0 && !sp.single) sp.single = paged_items(sp, (float)units * capf, (int)units, capf) == 0;
+  sp.fixed = sp.single ? (int)cap : 0;
   size_t cur = 0;
   const int64_t rows = p.sp.single ? 0 : (int64_t)p.sp.n_items * p.rows;
   p.off_part_o = carve(cur, sizeof(float) * rows * d->head_dim);

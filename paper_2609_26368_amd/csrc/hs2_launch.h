@@ -1,6 +1,7 @@
 // Internal interface between the C ABI (hs2_api.hip) and the kernels.
 #pragma once
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -187,12 +188,59 @@ struct PagedPool {
 };
 
 // Splits of the paged attention, in blocks of 16 tokens: fixed > 0 fixes their
-// length (single: one a KV head, the grid's workgroups are the KV heads); else
-// every workgroup derives it from len[] (paged_split_blocks).
+// length (single: one a KV head, the grid's workgroups are the KV heads, no
+// merge is launched); else every workgroup derives it from len[]
+// (paged_split_blocks).
+//
+// The estimate of a call's time, in the time that a block takes a workgroup
+// while all of them stream (0.5 - 0.7 us): with `resident` workgroups at once, a
+// workgroup alone takes its blocks `alone` times faster; what a split costs
+// besides its blocks (its start, its partial written and read again) is
+// `item` blocks, the merge's launch `merge`.  A third of the longest item's time
+// is left over at the end, less where the device is filled in one round with
+// splits of one length: by few KV heads, or by sequences of one length.  Measured, us, one split a KV head / as many splits as
+// resident workgroups / 2 / 4 times as many: 512 KV heads of 1000-12000 tokens 304 /
+// 329 / 286 / 285, of 6000 243 / 247 / 250 / 254, 1600 of 100-2000 146 / 157 / 158 / 166,
+// 64 of 30000 316 / 158 / 158 / 158; 64 rows of head dim 256, 256 heads of 1500 71 / 82
+// / 103 / 135, 200 of 1000-4000 152 / 179 / 132 / 158.
 struct PagedSplit {
-  int fixed, align, min_blocks, n_items, few_items, cap_blocks;
+  int fixed, align, min_blocks, n_items, few_items, cap_blocks, resident;
   bool single;
+  float alone, item, merge;
 };
+__host__ __device__ inline float paged_time(const PagedSplit& sp, float total, float longest, float left) {
+  const float t = total / (float)sp.resident, last = longest / sp.alone;
+  return (t > last ? t : last) + left * last;
+}
+// The (sequence, KV head, split) items that the splits may number at most, 0: one
+// for each of the `units` KV heads.  total: blocks of all, longest: of one.
+__host__ __device__ inline int paged_items(const PagedSplit& sp, float total, int units, float longest) {
+  constexpr float LEFT = 0.35f;
+  float best = paged_time(sp, total, longest, LEFT);
+  int n = 0;
+  auto consider = [&](int items, float least, float left) {
+    const float u = 0.5f * (float)units;  // a KV head's last split is half full
+    const float s = total / ((float)items - u > 1.f ? (float)items - u : 1.f), S = s > least ? s : least;
+    const float all = total / S + u;
+    const float t = paged_time(sp, total + sp.item * (all < (float)items ? all : (float)items), S, left) + sp.merge;
+    if (t < best) {
+      best = t;
+      n = items;
+    }
+  };
+  // few tokens: short splits, at most one item per compute unit
+  if (sp.few_items > units && total <= (float)sp.min_blocks * (float)sp.few_items) {
+    consider(sp.few_items, (float)sp.align, LEFT);
+  } else {
+    const float many = fminf(1.f, 2.f * (float)units / (float)sp.resident);
+    const float ragged = fminf(1.f, longest * (float)units / fmaxf(total, 1.f) - 0.75f);
+    for (int k = 1; k <= 4; k *= 2) {
+      const int more = units + sp.resident / 4, items = k * sp.resident > more ? k * sp.resident : more;
+      consider(items < sp.n_items ? items : sp.n_items, (float)sp.min_blocks, k == 1 ? LEFT * many * ragged : LEFT);
+    }
+  }
+  return n;
+}
 
 struct PagedAttnArgs {
   PagedPool p;

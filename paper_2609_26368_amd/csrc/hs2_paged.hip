@@ -81,23 +81,33 @@ __device__ inline int wave_sum_sequences(const PagedAttnArgs& a, int n0, F&& f) 
 }
 __device__ inline int splits_at(int n, int S) { return max(1, (n + S - 1) / S); }
 
-// Blocks per split: the shortest multiple of align, at least min_blocks, whose
-// (sequence, KV head, split) items number at most n_items (few tokens: at
-// most few_items, with splits down to align).  items(S) lies between total / S and total / S +
-// units, which brackets the search.
-__device__ inline int paged_split_blocks(const PagedAttnArgs& a, int n0) {
+// Blocks per split, 0 if workgroup `item` has nothing to do.  Either the longest
+// sequence's (every KV head is one split), or the shortest multiple of align, at
+// least min_blocks, whose (sequence, KV head, split) items number at most what
+// paged_items says (few tokens: down to align).  items(S) lies between total / S
+// and total / S + units, which brackets the search.
+__device__ inline int paged_split_blocks(const PagedAttnArgs& a, int n0, int item) {
   const PagedSplit& sp = a.sp;
   if (sp.fixed) return sp.fixed;
   const int units = a.p.B * a.p.Hkv;
   float tot = 0.f;
+  int longest = 0;
   {
     const int lane = threadIdx.x & 63;
-    if (lane < a.p.B) tot = (float)n0;
-    for (int b = lane + 64; b < a.p.B; b += 64) tot += (float)paged_span(a, paged_len(a.p, b)).n;
+    if (lane < a.p.B) tot = (float)(longest = n0);
+    for (int b = lane + 64; b < a.p.B; b += 64) {
+      const int n = paged_span(a, paged_len(a.p, b)).n;
+      tot += (float)n;
+      longest = max(longest, n);
+    }
     tot = wave_sum(tot) * (float)a.p.Hkv;
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) longest = max(longest, __shfl_xor(longest, w));
   }
-  const bool few = sp.few_items > units && tot <= (float)sp.min_blocks * (float)sp.few_items;
-  const int n_items = few ? sp.few_items : sp.n_items;
+  const int n_items = paged_items(sp, tot, units, (float)longest);
+  if (n_items == 0) return item < units ? max(1, longest) : 0;
+  if (item >= n_items) return 0;
+  const bool few = n_items == sp.few_items && tot <= (float)sp.min_blocks * (float)n_items;
   const float n = (float)n_items, al = (float)sp.align;
   int lo = max(few ? 1 : sp.min_blocks / sp.align, (int)(tot * (0.9999f / (n * al))));
   int hi = (sp.cap_blocks + sp.align - 1) / sp.align;
@@ -331,10 +341,7 @@ __device__ inline void paged_store4(float4 o, float Z, float v_scale, const uint
 }
 
 template <int RPW, int NWV, int TGW, int TW, int NS, bool KV8, int HDIM, bool NTL>
-#ifndef WPE
-#define WPE 1
-#endif
-__global__ __launch_bounds__(64 * NWV * TGW, WPE) void k_paged_attn(PagedAttnArgs a) {
+__global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) {
   using P = PagedShape<RPW, NWV, TGW, TW, NS, KV8, HDIM>;
   constexpr int NB = TW / 16, NKK = HDIM / 32, RB = P::RB, SB = P::SB, LPM = P::LPM, CPR = RB / 16, RPL = 1024 / RB;
   constexpr int SRB = 2 * HDIM, NTH = 64 * P::NW, ROWS = P::ROWS, IDS = P::IDS;
@@ -352,8 +359,8 @@ __global__ __launch_bounds__(64 * NWV * TGW, WPE) void k_paged_attn(PagedAttnArg
     S = a.sp.fixed;
   } else {
     const int n0 = lane < a.p.B ? paged_span(a, paged_len(a.p, lane)).n : 0;
-    S = __builtin_amdgcn_readfirstlane(paged_split_blocks(a, n0));
-    if (!paged_locate(a, n0, S, blockIdx.x, it)) return;
+    S = __builtin_amdgcn_readfirstlane(paged_split_blocks(a, n0, blockIdx.x));
+    if (S == 0 || !paged_locate(a, n0, S, blockIdx.x, it)) return;
   }
   const int b = __builtin_amdgcn_readfirstlane(it.b), g = __builtin_amdgcn_readfirstlane(it.g);
   const int split = __builtin_amdgcn_readfirstlane(it.split), n_splits = __builtin_amdgcn_readfirstlane(it.n_splits);
@@ -423,9 +430,17 @@ __global__ __launch_bounds__(64 * NWV * TGW, WPE) void k_paged_attn(PagedAttnArg
     const int e = tile * NB + lane;                     // block of the group
     const int T = (e / NB) * TGW + tg, i = T * NB + e % NB;  // tile and block of the split
     uint4 d = make_uint4(0, 0, NONE, 0);
+    // (without a window the entry is known, and loaded, before the length is)
+    const int v = i0 + i, most = a.p.max_pages - 1;
+    int t0, id;
+    if (a.window == 0) {
+      t0 = 16 * v;
+      id = a.p.table[(int64_t)b * a.p.max_pages + min(t0 >> a.p.page_shift, most)];
+    } else {
+      t0 = 16 * token_block(span, v);
+      id = a.p.table[(int64_t)b * a.p.max_pages + min(max(t0 >> a.p.page_shift, 0), most)];
+    }
     if (i < n_blocks) {
-      const int v = i0 + i, t0 = 16 * token_block(span, v);
-      const int id = a.p.table[(int64_t)b * a.p.max_pages + (t0 >> a.p.page_shift)];
       if (is_page(id, a.p.n_pages)) {
         const int64_t off = id * a.p.stride_p + (t0 & (a.p.page - 1)) * a.p.stride_t;
         const int lo = t0 < a.first ? 0 : max(0, span.lo - t0);
@@ -1177,14 +1192,14 @@ __global__ __launch_bounds__(NTP) void k_pages_copy(PagesCopyArgs a) {
 // dim, row tiles per wave, waves per ring, token groups, rows and stages of a
 // ring.
 #ifndef HS2_PAGED_SHAPES
-#define HS2_PAGED_SHAPES(X)                                            \
-  X(1, false, 128, 1, 1, 4, 16, 2) X(2, false, 128, 2, 1, 4, 16, 2)    \
-  X(4, false, 128, 2, 2, 2, 32, 2) X(8, false, 128, 2, 4, 1, 32, 2)    \
-  X(1, false, 256, 1, 1, 4, 16, 2) X(2, false, 256, 1, 2, 2, 32, 2)    \
-  X(4, false, 256, 1, 4, 1, 32, 3) X(8, false, 256, 1, 8, 1, 32, 4)    \
-  X(1, true, 128, 1, 1, 4, 32, 2) X(2, true, 128, 2, 1, 4, 32, 2)      \
-  X(4, true, 128, 2, 2, 2, 32, 2) X(8, true, 128, 2, 4, 1, 32, 2)      \
-  X(1, true, 256, 1, 1, 4, 16, 2) X(2, true, 256, 1, 2, 2, 32, 2)      \
+#define HS2_PAGED_SHAPES(X)                                                        \
+  X(1, false, 128, 1, 1, 4, 16, 2) X(2, false, 128, 2, 1, 4, 16, 2)          \
+  X(4, false, 128, 2, 2, 2, 32, 2) X(8, false, 128, 2, 4, 1, 32, 2)          \
+  X(1, false, 256, 1, 1, 4, 16, 2) X(2, false, 256, 1, 2, 2, 32, 2)          \
+  X(4, false, 256, 1, 4, 1, 32, 3) X(8, false, 256, 1, 8, 1, 32, 4)          \
+  X(1, true, 128, 1, 1, 4, 32, 2) X(2, true, 128, 2, 1, 4, 32, 2)            \
+  X(4, true, 128, 2, 2, 2, 32, 2) X(8, true, 128, 2, 4, 1, 32, 2)            \
+  X(1, true, 256, 1, 1, 4, 16, 2) X(2, true, 256, 1, 2, 2, 32, 2)            \
   X(4, true, 256, 1, 4, 1, 32, 2) X(8, true, 256, 1, 8, 1, 32, 4)
 #endif
 
