@@ -54,8 +54,10 @@
  * HS2_FA_CACHE_POLICY (0: every full-attention load cacheable, 1: V rows
  * non-temporal, 2: K and V non-temporal, 3: V and the leading K rows of
  * each token group non-temporal; 1 and 2 exist for one query row tile, 3
- * for more) and HS2_FA_K_KEEP (percent of each token group's K rows that
- * policy 3 keeps cacheable).  None changes a result beyond floating-point
+ * for more), HS2_FA_K_KEEP (percent of each token group's K rows that
+ * policy 3 keeps cacheable) and HS2_PAGED_STREAM (paged attention: 0 every
+ * pool row cacheable, 1 rows of pages that no neighbouring sequence shares
+ * non-temporal).  None changes a result beyond floating-point
  * summation order; the cache policies change none at all.
  */
 #ifndef HS2_H

@@ -11,6 +11,7 @@
 //   k_pages_copy     the moves' contents
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 #include "hs2_device.h"
 #include "hs2_launch.h"
@@ -310,7 +311,9 @@ struct PagedShape {
   // us, with shared tiles 142)
   static constexpr bool KCONV = KV8 && NWV > 2;
   static constexpr int GB = NS * SB + (KCONV ? 2 * TW * 2 * HDIM : 0);
-  static constexpr int IDS = NW > 4 ? 64 : 128;          // blocks described per wave, two halves
+  // blocks described per wave, in two halves (a refill waits for every load in
+  // flight); where the ring leaves room for one workgroup only, more
+  static constexpr int IDS = TGW * GB > 80 * 1024 && NW == 4 ? 256 : 128;
   // columns per exchange of the groups' outputs
   static constexpr int CW = TGW * ROWS * (HDIM + 4) * 4 <= (TGW * GB > 70000 ? TGW * GB : 70000) ? HDIM : HDIM / 2;
   static constexpr int EXCH = TGW * ROWS * (CW + 4) * 4;
@@ -340,7 +343,7 @@ __device__ inline void paged_store4(float4 o, float Z, float v_scale, const uint
   *(uint2*)out = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
 }
 
-template <int RPW, int NWV, int TGW, int TW, int NS, bool KV8, int HDIM, bool NTL>
+template <int RPW, int NWV, int TGW, int TW, int NS, bool KV8, int HDIM>
 __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) {
   using P = PagedShape<RPW, NWV, TGW, TW, NS, KV8, HDIM>;
   constexpr int NB = TW / 16, NKK = HDIM / 32, RB = P::RB, SB = P::SB, LPM = P::LPM, CPR = RB / 16, RPL = 1024 / RB;
@@ -421,34 +424,49 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
   auto sees = [&](int pos, int t) { return t <= pos && (a.window == 0 || t > pos - a.window || t < a.first); };
   bool deferred = false;
 
-  // Blocks are described 64 at a time, a lane each, in LDS: x, y: byte offset of
+  // Blocks are described IDS / 2 at a time, a lane each, in LDS: x, y: byte offset of
   // the first row in the pool; z: the rows [lo, hi] that some query sees, lo +
   // 256 hi (rows outside repeat one of them), or NONE (zero rows: no page); w:
-  // first token.  The loop over tiles then needs a few scalars a block.
-  constexpr uint32_t ALL = 15u << 8, NONE = 16u;
+  // first token, and CACHED.  The loop over tiles then needs a few scalars a block.
+  //
+  // Rows of pools past the last-level cache are read non-temporal (64 sequences
+  // of 8000 tokens 351 -> 310 us) but for pages that the sequence before or
+  // behind has too (a common prompt, beams), which the caches are to keep for it
+  // (4 beams each sharing nine tenths 195 us non-temporal, 163 cacheable).
+  constexpr uint32_t ALL = 15u << 8, NONE = 16u, CACHED = 1u << 31;
   auto describe = [&](int tile) __attribute__((always_inline)) {
-    const int e = tile * NB + lane;                     // block of the group
-    const int T = (e / NB) * TGW + tg, i = T * NB + e % NB;  // tile and block of the split
-    uint4 d = make_uint4(0, 0, NONE, 0);
-    // (without a window the entry is known, and loaded, before the length is)
-    const int v = i0 + i, most = a.p.max_pages - 1;
-    int t0, id;
-    if (a.window == 0) {
-      t0 = 16 * v;
-      id = a.p.table[(int64_t)b * a.p.max_pages + min(t0 >> a.p.page_shift, most)];
-    } else {
-      t0 = 16 * token_block(span, v);
-      id = a.p.table[(int64_t)b * a.p.max_pages + min(max(t0 >> a.p.page_shift, 0), most)];
-    }
-    if (i < n_blocks) {
-      if (is_page(id, a.p.n_pages)) {
-        const int64_t off = id * a.p.stride_p + (t0 & (a.p.page - 1)) * a.p.stride_t;
-        const int lo = t0 < a.first ? 0 : max(0, span.lo - t0);
-        const int hi = min(15, (v < span.nf ? min(a.first, Lv) : Lv) - 1 - t0);
-        d = make_uint4((uint32_t)off, (uint32_t)(off >> 32), (uint32_t)(lo | hi << 8), (uint32_t)t0);
+#pragma unroll
+    for (int more = 0; more < IDS / 128; ++more) {
+      const int e = tile * NB + 64 * more + lane;         // block of the group
+      const int T = (e / NB) * TGW + tg, i = T * NB + e % NB;  // tile and block of the split
+      uint4 d = make_uint4(0, 0, NONE, 0);
+      // (without a window the entry is known, and loaded, before the length is)
+      const int v = i0 + i, most = a.p.max_pages - 1;
+      int t0;
+      const int32_t* entry = a.p.table + (int64_t)b * a.p.max_pages;
+      if (a.window == 0) {
+        t0 = 16 * v;
+        entry += min(t0 >> a.p.page_shift, most);
+      } else {
+        t0 = 16 * token_block(span, v);
+        entry += min(max(t0 >> a.p.page_shift, 0), most);
       }
+      const int id = *entry;
+      uint32_t cached = CACHED;
+      if (a.stream) {
+        const int before = b > 0 ? entry[-(int64_t)a.p.max_pages] : -1, behind = b + 1 < a.p.B ? entry[a.p.max_pages] : -1;
+        if (id != before && id != behind) cached = 0;
+      }
+      if (i < n_blocks) {
+        if (is_page(id, a.p.n_pages)) {
+          const int64_t off = id * a.p.stride_p + (t0 & (a.p.page - 1)) * a.p.stride_t;
+          const int lo = t0 < a.first ? 0 : max(0, span.lo - t0);
+          const int hi = min(15, (v < span.nf ? min(a.first, Lv) : Lv) - 1 - t0);
+          d = make_uint4((uint32_t)off, (uint32_t)(off >> 32), (uint32_t)(lo | hi << 8), (uint32_t)t0 | cached);
+        }
+      }
+      blocks[e % IDS] = d;
     }
-    if (IDS == 128 || lane < IDS / 2) blocks[e % IDS] = d;
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
     asm volatile("" ::: "memory");
   };
@@ -467,34 +485,47 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
     lane_off[u] = lane_offset(row, row & 15);
   }
   // (every stage issues all its loads: the waits count them)
+  constexpr int WB = NWV > 1 ? 1 : NB;                // blocks that a wave loads rows of
+  const int wb0 = NWV > 1 ? wave * NB / NWV : 0;      // its first
+  static_assert(NWV == 1 || NWV % NB == 0, "a wave's rows are of one block");
   auto issue_to = [&](int tile, int stage) __attribute__((always_inline)) {
-    const uint32_t base = ring + (uint32_t)(stage * SB);
-    const unsigned char *kp[NB], *vp[NB];
-    uint32_t z[NB];
+    const uint32_t base = ring + (uint32_t)(stage * SB) + 1024u * (uint32_t)(wave * LPM);
+    const unsigned char *kp[WB], *vp[WB];
+    uint32_t z[WB], cached = 0;
     bool all = true;
 #pragma unroll
-    for (int bi = 0; bi < NB; ++bi) {
-      const uint4 d = blocks[(tile * NB + bi) % IDS];
-      z[bi] = (uint32_t)__builtin_amdgcn_readfirstlane(d.z);
+    for (int k = 0; k < WB; ++k) {
+      const uint4 d = blocks[(tile * NB + wb0 + k) % IDS];
+      z[k] = (uint32_t)__builtin_amdgcn_readfirstlane(d.z);
+      cached |= (uint32_t)__builtin_amdgcn_readfirstlane(d.w);
       const uint64_t off = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(d.x) |
                            (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(d.y) << 32;
-      kp[bi] = z[bi] == NONE ? (const unsigned char*)zero_row : Kg + off;
-      vp[bi] = z[bi] == NONE ? (const unsigned char*)zero_row : Vg + off;
-      all &= z[bi] == ALL;
+      kp[k] = z[k] == NONE ? (const unsigned char*)zero_row : Kg + off;
+      vp[k] = z[k] == NONE ? (const unsigned char*)zero_row : Vg + off;
+      all &= z[k] == ALL;
     }
+    uint32_t from[LPM];
 #pragma unroll
     for (int u = 0; u < LPM; ++u) {
-      const int n = wave * LPM + u;
-      const bool second = NB > 1 && (RPL * n) / 16 == 1;
-      uint32_t lo = lane_off[u];
+      from[u] = lane_off[u];
       if (!all) {
-        const int row = RPL * n + lrow;
-        const uint32_t r = second ? z[NB - 1] : z[0];
-        lo = lane_offset(row, r == NONE ? 0 : max((int)(r & 255u), min(row & 15, (int)(r >> 8))));
+        const int row = RPL * (wave * LPM + u) + lrow;
+        const uint32_t r = z[WB > 1 ? RPL * u / 16 : 0];
+        from[u] = lane_offset(row, r == NONE ? 0 : max((int)(r & 255u), min(row & 15, (int)(r >> 8))));
       }
-      dma16_s<NTL>(second ? kp[NB - 1] : kp[0], lo, __builtin_amdgcn_readfirstlane(base + 1024 * n));
-      dma16_s<NTL>(second ? vp[NB - 1] : vp[0], lo, __builtin_amdgcn_readfirstlane(base + TW * RB + 1024 * n));
     }
+    auto load = [&](auto nt) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < LPM; ++u) {
+        const int k = WB > 1 ? RPL * u / 16 : 0;
+        dma16_s<decltype(nt)::value>(kp[k], from[u], __builtin_amdgcn_readfirstlane(base + 1024 * u));
+        dma16_s<decltype(nt)::value>(vp[k], from[u], __builtin_amdgcn_readfirstlane(base + TW * RB + 1024 * u));
+      }
+    };
+    if (!(cached & CACHED))
+      load(std::true_type{});
+    else
+      load(std::false_type{});
   };
   auto issue = [&](int tile) __attribute__((always_inline)) {
     if (tile % (IDS / 2 / NB) == 0) describe(tile);
@@ -565,7 +596,7 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
       if (apart) {
 #pragma unroll
         for (int bi = 0; bi < NB; ++bi) {
-          const int t0 = __builtin_amdgcn_readfirstlane(blocks[(i * NB + bi) % IDS].w) + 4 * (lane >> 4);
+          const int t0 = (int)(__builtin_amdgcn_readfirstlane(blocks[(i * NB + bi) % IDS].w) & ~CACHED) + 4 * (lane >> 4);
 #pragma unroll
           for (int rr = 0; rr < RPW; ++rr) {
             const int pos = Lv - a.C + min((16 * (rt0 + rr) + (lane & 15)) / a.Gp, a.C - 1);
@@ -629,7 +660,7 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
       bool there[NB];
 #pragma unroll
       for (int bi = 0; bi < NB; ++bi) {
-        t0[bi] = __builtin_amdgcn_readfirstlane(blocks[(i * NB + bi) % IDS].w) + 4 * (lane >> 4);
+        t0[bi] = (int)(__builtin_amdgcn_readfirstlane(blocks[(i * NB + bi) % IDS].w) & ~CACHED) + 4 * (lane >> 4);
         there[bi] = rows_of(i, bi) != NONE;
       }
 #pragma unroll
@@ -1225,7 +1256,7 @@ hipError_t paged_attn_wgs(int RT, bool kv8, int hd, int* wgs) {
   if (RT == rt && kv8 == f8 && hd == hdim) {                                                              \
     using P = PagedShape<rpw, nwv, tgw, tw, ns, f8, hdim>;                                                \
     const hipError_t e = hipOccupancyMaxActiveBlocksPerMultiprocessor(                                    \
-        wgs, (const void*)k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim, true>, 64 * P::NW, P::LDS);       \
+        wgs, (const void*)k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim>, 64 * P::NW, P::LDS);       \
     *wgs = std::min(*wgs, 160 * 1024 / (P::LDS_ALL + 1024));                                              \
     return e;                                                                                             \
   }
@@ -1234,19 +1265,13 @@ hipError_t paged_attn_wgs(int RT, bool kv8, int hd, int* wgs) {
   return hipErrorInvalidValue;
 }
 
-template <int LDS>
-static hipError_t paged_allow_lds(const void* cached, const void* streamed) {
-  const hipError_t e = hipFuncSetAttribute(cached, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-  return e != hipSuccess ? e : hipFuncSetAttribute(streamed, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-}
-
 hipError_t set_paged_smem_limits() {
   hipError_t e = hipSuccess;
 #define HS2_PAGED_ATTR(rt, f8, hdim, rpw, nwv, tgw, tw, ns)                                               \
   if (e == hipSuccess)                                                                                    \
-    e = paged_allow_lds<PagedShape<rpw, nwv, tgw, tw, ns, f8, hdim>::LDS>(                                \
-        (const void*)k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim, false>,                                \
-        (const void*)k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim, true>);
+    e = hipFuncSetAttribute((const void*)k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim>,                   \
+                            hipFuncAttributeMaxDynamicSharedMemorySize,                                   \
+                            PagedShape<rpw, nwv, tgw, tw, ns, f8, hdim>::LDS);
   HS2_PAGED_SHAPES(HS2_PAGED_ATTR)
 #undef HS2_PAGED_ATTR
   return e;
@@ -1258,10 +1283,7 @@ hipError_t launch_paged_attn(const PagedAttnArgs& a, int RT, hipStream_t s) {
 #define HS2_PAGED_LAUNCH(rt, f8, hdim, rpw, nwv, tgw, tw, ns)                                             \
   if (RT == rt && kv8 == f8 && a.p.hd == hdim) {                                                          \
     using P = PagedShape<rpw, nwv, tgw, tw, ns, f8, hdim>;                                                \
-    if (a.stream)                                                                                         \
-      k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim, true><<<grid, 64 * P::NW, P::LDS, s>>>(a);            \
-    else                                                                                                  \
-      k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim, false><<<grid, 64 * P::NW, P::LDS, s>>>(a);           \
+    k_paged_attn<rpw, nwv, tgw, tw, ns, f8, hdim><<<grid, 64 * P::NW, P::LDS, s>>>(a);                    \
     return hipGetLastError();                                                                             \
   }
   HS2_PAGED_SHAPES(HS2_PAGED_LAUNCH)

@@ -219,6 +219,55 @@ def test_what_only_some_queries_see(kv, D, Hq, poison):
     assert torch.isfinite(out[0, 2:]).all() and not torch.isfinite(out[0, :2]).any()
 
 
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("Hq,D", [(8, 128), (32, 128), (8, 256), (64, 256)])
+@pytest.mark.parametrize("C", [1, 2])
+def test_tokens_that_nobody_sees_hold_nan(kv, Hq, D, C):
+    """Between the first tokens and the windows, also within one 16-token block."""
+    window, first, lens = 5, 3, [9, 17, 20, 30, 47, 250]
+    s = Setup(21, kv, D, 1, 16, lens, layout="record")
+    bad = 0x7F if kv == "e4m3" else math.nan
+    for b, L in enumerate(lens):
+        seen = set(np.concatenate([PO.visible(L - C + c, window, first) for c in range(C)]).tolist())
+        for t in set(range(L)) - seen:
+            for X in (s.K, s.V):
+                X[int(s.table[b, t // 16]), :, t % 16] = bad
+    s.check(C, Hq, window=window, first=first)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("C,Hq,D", [(2, 8, 128), (3, 16, 128), (2, 64, 256), (16, 8, 128), (16, 8, 256)])
+def test_queries_apart(kv, C, Hq, D):
+    """Each query alone among tokens that only the others of the chunk see, all of them NaN."""
+    L, window, first = 90, 21, 2
+    bad = 0x7F if kv == "e4m3" else math.nan
+    for c in range(0, C, max(1, C // 4)):
+        s = Setup(22, kv, D, 1, 16, [L], layout="token")
+        q, sink, gate = s.queries(C, Hq, True)
+        want, weight = s.reference(q, sink, gate, window, first)
+        seen = set(PO.visible(L - C + c, window, first).tolist())
+        for t in set(range(L)) - seen:
+            for X in (s.K, s.V):
+                X[int(s.table[0, t // 16]), :, t % 16] = bad
+        out = s.attend(q, sink, gate, window, first)
+        check_out(out[:, c], want[:, c], weight[:, c], f"query {c}")
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("C,Hq,D", [(1, 8, 128), (2, 32, 128), (1, 64, 256)])
+def test_cache_policies_give_the_same_bits(kv, C, Hq, D, monkeypatch):
+    s = Setup(23, kv, D, 2, 16, [3000, 3000, 40, 700, 3001], layout="record")
+    s.table[1, :100] = s.table[0, :100]  # a common prompt
+    s.dtable = torch.from_numpy(s.table).cuda()
+    q, sink, gate = s.queries(C, Hq, True)
+    outs = []
+    for v in ("0", "1"):
+        monkeypatch.setenv("HS2_PAGED_STREAM", v)
+        outs.append((s.attend(q, sink, gate), s.attend(q, sink, gate, 1000, 5)))
+    assert all(torch.equal(x, y) for x, y in zip(*outs))
+    check_out(outs[1][0], *s.reference(q, sink, gate))
+
+
 def test_negative_and_excessive_lengths():
     s = Setup(13, "bf16", 128, 2, 16, [100, 100, 112], max_pages=7)
     q, _, _ = s.queries(1, 8, False)
