@@ -1103,7 +1103,7 @@ hs2_status paged_attn_impl(const hs2_paged_dims* d, const uint16_t* q, const voi
   const PagedPlan plan = paged_plan(d, kv8, window, first, di);
   if (workspace_bytes < plan.bytes)
     return fail(HS2_ERR_WORKSPACE, "workspace %zu bytes < %zu required", workspace_bytes, plan.bytes);
-  if ((st = ensure_device_init(&di)) != HS2_OK) return st;
+  if (!di && (st = ensure_device_init(&di)) != HS2_OK) return st;
   PagedAttnArgs a{};
   a.p = paged_pool(d, K, V, table, len, kv8 ? 1 : 2);
   a.sp = plan.sp;
@@ -1119,7 +1119,7 @@ hs2_status paged_attn_impl(const hs2_paged_dims* d, const uint16_t* q, const voi
   a.C = d->n_queries;
   a.Hq = d->n_q_heads;
   a.G = d->n_q_heads / d->n_kv_heads;
-  a.Gp = next_pow2(a.G);
+  a.gp_shift = ilog2(next_pow2(a.G));
   a.window = window;
   a.first = first;
   // rows that the last-level cache cannot hold until the next step stream past it

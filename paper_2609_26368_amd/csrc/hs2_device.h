@@ -118,6 +118,16 @@ __device__ inline int wave_scan(int v) {
   return v;
 }
 __device__ inline int wave_sum(int v) { return __builtin_amdgcn_readlane(wave_scan(v), 63); }
+// largest of the wave's values, all >= 0
+__device__ inline int wave_max(int v) {
+  v = max(v, dpp_move<0x111, 0xF>(v));
+  v = max(v, dpp_move<0x112, 0xF>(v));
+  v = max(v, dpp_move<0x114, 0xF>(v));
+  v = max(v, dpp_move<0x118, 0xF>(v));
+  v = max(v, dpp_move<0x142, 0xA>(v));
+  v = max(v, dpp_move<0x143, 0xC>(v));
+  return __builtin_amdgcn_readlane(v, 63);
+}
 __device__ inline float wave_sum(float v) {
   auto add = [](float a, int b) { return a + __int_as_float(b); };
   v = add(v, dpp_move<0x111, 0xF>(__float_as_int(v)));

@@ -208,8 +208,15 @@ struct PagedSplit {
   bool single;
   float alone, item, merge;
 };
+__host__ __device__ inline float paged_over(float x, float y) {  // x / y, nearly
+#ifdef __HIP_DEVICE_COMPILE__
+  return x * __builtin_amdgcn_rcpf(y);
+#else
+  return x / y;
+#endif
+}
 __host__ __device__ inline float paged_time(const PagedSplit& sp, float total, float longest, float left) {
-  const float t = total / (float)sp.resident, last = longest / sp.alone;
+  const float t = paged_over(total, (float)sp.resident), last = paged_over(longest, sp.alone);
   return (t > last ? t : last) + left * last;
 }
 // The (sequence, KV head, split) items that the splits may number at most, 0: one
@@ -220,8 +227,8 @@ __host__ __device__ inline int paged_items(const PagedSplit& sp, float total, in
   int n = 0;
   auto consider = [&](int items, float least, float left) {
     const float u = 0.5f * (float)units;  // a KV head's last split is half full
-    const float s = total / ((float)items - u > 1.f ? (float)items - u : 1.f), S = s > least ? s : least;
-    const float all = total / S + u;
+    const float s = paged_over(total, (float)items - u > 1.f ? (float)items - u : 1.f), S = s > least ? s : least;
+    const float all = paged_over(total, S) + u;
     const float t = paged_time(sp, total + sp.item * (all < (float)items ? all : (float)items), S, left) + sp.merge;
     if (t < best) {
       best = t;
@@ -232,8 +239,8 @@ __host__ __device__ inline int paged_items(const PagedSplit& sp, float total, in
   if (sp.few_items > units && total <= (float)sp.min_blocks * (float)sp.few_items) {
     consider(sp.few_items, (float)sp.align, LEFT);
   } else {
-    const float many = fminf(1.f, 2.f * (float)units / (float)sp.resident);
-    const float ragged = fminf(1.f, longest * (float)units / fmaxf(total, 1.f) - 0.75f);
+    const float many = fminf(1.f, paged_over(2.f * (float)units, (float)sp.resident));
+    const float ragged = fminf(1.f, paged_over(longest * (float)units, fmaxf(total, 1.f)) - 0.75f);
     for (int k = 1; k <= 4; k *= 2) {
       const int more = units + sp.resident / 4, items = k * sp.resident > more ? k * sp.resident : more;
       consider(items < sp.n_items ? items : sp.n_items, (float)sp.min_blocks, k == 1 ? LEFT * many * ragged : LEFT);
@@ -252,7 +259,7 @@ struct PagedAttnArgs {
   const uint16_t* q;
   uint16_t* out;           // [B, C, Hq, hd]
   float c2;                // softmax scale * log2(e)
-  int C, Hq, G, Gp;
+  int C, Hq, G, gp_shift;  // query rows c * 2^gp_shift + h
   int window, first;       // window 0: every token is seen
   int stream;              // pool rows are read non-temporal
   const float* k_scale;    // [Hkv] for an E4M3 pool, else null

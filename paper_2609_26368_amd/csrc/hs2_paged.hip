@@ -80,7 +80,7 @@ __device__ inline int wave_sum_sequences(const PagedAttnArgs& a, int n0, F&& f) 
   for (int b = lane + 64; b < a.p.B; b += 64) s += f(paged_span(a, paged_len(a.p, b)).n);
   return wave_sum(s);
 }
-__device__ inline int splits_at(int n, int S) { return max(1, (n + S - 1) / S); }
+__device__ inline int splits_at(int n, int S) { return max(1, (int)((uint32_t)(n + S - 1) / (uint32_t)S)); }
 
 // Blocks per split, 0 if workgroup `item` has nothing to do.  Either the longest
 // sequence's (every KV head is one split), or the shortest multiple of align, at
@@ -102,8 +102,7 @@ __device__ inline int paged_split_blocks(const PagedAttnArgs& a, int n0, int ite
       longest = max(longest, n);
     }
     tot = wave_sum(tot) * (float)a.p.Hkv;
-#pragma unroll
-    for (int w = 1; w < 64; w *= 2) longest = max(longest, __shfl_xor(longest, w));
+    longest = wave_max(longest);
   }
   const int n_items = paged_items(sp, tot, units, (float)longest);
   if (n_items == 0) return item < units ? max(1, longest) : 0;
@@ -142,8 +141,8 @@ __device__ inline bool paged_locate(const PagedAttnArgs& a, int n0, int S, int i
       it.n_splits = __builtin_amdgcn_readlane(k, l);
       const int r = item - (__builtin_amdgcn_readlane(incl, l) - it.n_splits * a.p.Hkv);
       it.b = b0 + l;
-      it.g = r / it.n_splits;
-      it.split = r % it.n_splits;
+      it.g = (int)((uint32_t)r / (uint32_t)it.n_splits);
+      it.split = r - it.g * it.n_splits;
       return true;
     }
     item -= __builtin_amdgcn_readlane(incl, 63);
@@ -256,7 +255,7 @@ __device__ inline uint4 v_operand(const unsigned char* v, int i, int nb, int lan
 // seen(bi, j, c): whether query c sees the lane's token j of block bi.
 template <int RPW, int NB, int HDIM, bool KV8, int RB, class Seen>
 __device__ inline void pv_apart(PagedState<RPW, HDIM>& st, const PFrags<NB, RPW>& pf, const unsigned char* v, int C,
-                                int Gp, int rt0, int lane, Seen&& seen) {
+                                int gp_shift, int rt0, int lane, Seen&& seen) {
   constexpr bool K32 = NB % 2 == 0;
   int c = 0;
   do {
@@ -265,7 +264,7 @@ __device__ inline void pv_apart(PagedState<RPW, HDIM>& st, const PFrags<NB, RPW>
     for (int rr = 0; rr < RPW; ++rr)
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        mine[rr][k] = (16 * (rt0 + rr) + 4 * (lane >> 4) + k) / Gp == c ? 0xFFFFFFFFu : 0u;
+        mine[rr][k] = (16 * (rt0 + rr) + 4 * (lane >> 4) + k) >> gp_shift == c ? 0xFFFFFFFFu : 0u;
 #pragma unroll
     for (int i = 0; i < (K32 ? NB / 2 : NB); ++i) {
       uint32_t keep[4];  // of the lane's tokens, two a word, in the operand's order
@@ -319,7 +318,7 @@ struct PagedShape {
   static constexpr int EXCH = TGW * ROWS * (CW + 4) * 4;
   static constexpr int RING = TGW * GB > EXCH ? TGW * GB : EXCH;
   static constexpr int LDS = RING + NW * IDS * 16;
-  static constexpr int LDS_ALL = LDS + TGW * ROWS * 8;   // with the row statistics
+  static constexpr int LDS_ALL = LDS + TGW * ROWS * 8 + ROWS * 4;  // with the row statistics
   static_assert(LPM >= 1 && TW * RB == 1024 * LPM * NWV && TW <= 32, "whole 1 KB loads for every wave and stage, two blocks");
   static_assert(LDS_ALL <= 160 * 1024, "fits a compute unit");
 };
@@ -330,11 +329,10 @@ __device__ inline float merge_weight(float m, float M) { return m == -INFINITY ?
 
 // Four columns of a finished row: over Z, times the cache's scale and the
 // gate's sigmoid, rounded to bf16.
-__device__ inline void paged_store4(float4 o, float Z, float v_scale, const uint16_t* gate, uint16_t* out) {
+__device__ inline void paged_store4(float4 o, float Z, float v_scale, bool gated, uint2 gb, uint16_t* out) {
   const float inv = (Z > 0.f || Z != Z ? 1.f / Z : 0.f) * v_scale;
   float x[4] = {o.x * inv, o.y * inv, o.z * inv, o.w * inv};
-  if (gate) {
-    const uint2 gb = *(const uint2*)gate;
+  if (gated) {
     const float gv[4] = {bf16_bits_to_f32(gb.x & 0xFFFFu), bf16_bits_to_f32(gb.x >> 16),
                          bf16_bits_to_f32(gb.y & 0xFFFFu), bf16_bits_to_f32(gb.y >> 16)};
 #pragma unroll
@@ -350,7 +348,7 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
   constexpr int SRB = 2 * HDIM, NTH = 64 * P::NW, ROWS = P::ROWS, IDS = P::IDS;
   constexpr bool KCONV = P::KCONV;
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ float s_m[TGW][ROWS], s_l[TGW][ROWS];
+  __shared__ float s_m[TGW][ROWS], s_l[TGW][ROWS], s_sink[ROWS];
 
   const int lane = threadIdx.x & 63;
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -358,7 +356,7 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
   PagedItem it;
   int S;
   if (a.sp.single) {  // one split per KV head
-    it = PagedItem{(int)blockIdx.x / a.p.Hkv, (int)blockIdx.x % a.p.Hkv, 0, 1};
+    it = PagedItem{(int)(blockIdx.x / (uint32_t)a.p.Hkv), (int)(blockIdx.x % (uint32_t)a.p.Hkv), 0, 1};
     S = a.sp.fixed;
   } else {
     const int n0 = lane < a.p.B ? paged_span(a, paged_len(a.p, lane)).n : 0;
@@ -379,7 +377,7 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
   uint4 q[RPW][NKK];
 #pragma unroll
   for (int rr = 0; rr < RPW; ++rr) {
-    const int r = 16 * (rt0 + rr) + (lane & 15), c = r / a.Gp, h = r % a.Gp;
+    const int r = 16 * (rt0 + rr) + (lane & 15), c = r >> a.gp_shift, h = r & ((1 << a.gp_shift) - 1);
     const bool real = c < a.C && h < a.G;
     const uint16_t* p = a.q + (((int64_t)b * a.C + (real ? c : 0)) * a.Hq + g * a.G + (real ? h : 0)) * HDIM;
 #pragma unroll
@@ -387,6 +385,11 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
       q[rr][kk] = *(const uint4*)(p + q_koff(kk, lane));
       if (!real) q[rr][kk] = make_uint4(0, 0, 0, 0);
     }
+  }
+  const bool whole = n_splits == 1;  // this workgroup writes the output
+  for (int r = threadIdx.x; r < ROWS; r += NTH) {
+    const int h = r & ((1 << a.gp_shift) - 1);
+    s_sink[r] = whole && a.sink && h < a.G ? a.sink[g * a.G + h] * 1.4426950408889634f : -INFINITY;
   }
   float c2 = KV8 ? a.c2 * a.k_scale[g] : a.c2;
   if (c2 < FLT_MIN) c2 = FLT_MIN;  // -inf times it stays -inf
@@ -599,7 +602,7 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
           const int t0 = (int)(__builtin_amdgcn_readfirstlane(blocks[(i * NB + bi) % IDS].w) & ~CACHED) + 4 * (lane >> 4);
 #pragma unroll
           for (int rr = 0; rr < RPW; ++rr) {
-            const int pos = Lv - a.C + min((16 * (rt0 + rr) + (lane & 15)) / a.Gp, a.C - 1);
+            const int pos = Lv - a.C + min((16 * (rt0 + rr) + (lane & 15)) >> a.gp_shift, a.C - 1);
 #pragma unroll
             for (int ii = 0; ii < 4; ++ii) Sx[bi][rr][ii] = !bad && sees(pos, t0 + ii) ? Sx[bi][rr][ii] : -INFINITY;
           }
@@ -665,7 +668,7 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
       }
 #pragma unroll
       for (int rr = 0; rr < RPW; ++rr) {
-        const int pos = Lv - a.C + min((16 * (rt0 + rr) + (lane & 15)) / a.Gp, a.C - 1);
+        const int pos = Lv - a.C + min((16 * (rt0 + rr) + (lane & 15)) >> a.gp_shift, a.C - 1);
 #pragma unroll
         for (int bi = 0; bi < NB; ++bi)
 #pragma unroll
@@ -675,7 +678,7 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
       PFrags<NB, RPW> pf;
       paged_softmax(st, Sx, c2, pf, lane);
       pv_apart<RPW, NB, HDIM, KV8 && !KCONV, RB>(
-          st, pf, KCONV ? tile_v : stg + TW * RB, a.C, a.Gp, rt0, lane,
+          st, pf, KCONV ? tile_v : stg + TW * RB, a.C, a.gp_shift, rt0, lane,
           [&](int bi, int j, int c) { return there[bi] && sees(Lv - a.C + c, t0[bi] + j); });
       __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the stage has been read
       asm volatile("" ::: "memory");
@@ -683,7 +686,28 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
 
   // the groups' rows against their common maximum, summed; with one split the
   // sink's logit takes part and the output is written
-  const bool whole = n_splits == 1;
+  constexpr int CW = P::CW, XS = CW + 4, NQ = CW / 4;
+  const int items = (a.C << a.gp_shift) * NQ;  // column quads of the rows
+  auto real_row = [&](int e, int& c, int& h) {
+    const int r = e / NQ;
+    c = r >> a.gp_shift;
+    h = r & ((1 << a.gp_shift) - 1);
+    return h < a.G;
+  };
+  auto out_at = [&](int e, int c, int h, int d0) {
+    return (((int64_t)b * a.C + c) * a.Hq + g * a.G + h) * HDIM + d0 + 4 * (e % NQ);
+  };
+  // gates on their way while the groups exchange their rows
+  constexpr int EPT = ROWS * NQ / NTH;
+  constexpr bool EARLY = EPT <= 4 && CW == HDIM;
+  uint2 gates[EARLY ? EPT : 1] = {};
+  if (EARLY && whole && a.gate)
+#pragma unroll
+    for (int k = 0; k < (EARLY ? EPT : 1); ++k) {
+      int c, h;
+      const int e = threadIdx.x + NTH * k;
+      if (e < items && real_row(e, c, h)) gates[k] = *(const uint2*)(a.gate + out_at(e, c, h, 0));
+    }
 #pragma unroll
   for (int rr = 0; rr < RPW; ++rr) {
     if (lane < 16) s_m[tg][16 * (rt0 + rr) + lane] = st.m[rr];
@@ -693,17 +717,12 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
   }
   const float v_scale = KV8 ? a.v_scale[g] : 1.f;
   __syncthreads();  // and every ring is free
-  auto sink_of = [&](int r) {
-    const int h = r % a.Gp;
-    return whole && a.sink && h < a.G ? a.sink[g * a.G + h] * 1.4426950408889634f : -INFINITY;
-  };
   auto row_max = [&](int r) {
-    float M = sink_of(r);
+    float M = s_sink[r];
 #pragma unroll
     for (int w = 0; w < TGW; ++w) M = fmaxf(M, s_m[w][r]);
     return M;
   };
-  constexpr int CW = P::CW, XS = CW + 4, NQ = CW / 4;
   float* xo = (float*)smem;  // [TGW][ROWS][XS]
 #pragma unroll
   for (int d0 = 0; d0 < HDIM; d0 += CW) {
@@ -713,18 +732,19 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r = 16 * (rt0 + rr) + 4 * (lane >> 4) + i;
-        const float M = row_max(r);
-        const float f = merge_weight(s_m[tg][r], M);
+        const float f = merge_weight(s_m[tg][r], row_max(r));
 #pragma unroll
         for (int nb = 0; nb < CW / 16; ++nb)
           xo[(tg * ROWS + r) * XS + 16 * nb + (lane & 15)] = st.o[rr][d0 / 16 + nb][i] * f;
       }
     __syncthreads();
-    for (int e = threadIdx.x; e < ROWS * NQ; e += NTH) {
-      const int r = e / NQ, d = 4 * (e % NQ), c = r / a.Gp, h = r % a.Gp;
-      if (c >= a.C || h >= a.G) continue;
-      const float sink = sink_of(r), M = row_max(r);
-      float Z = merge_weight(sink, M);
+#pragma unroll
+    for (int k = 0; k < EPT; ++k) {
+      const int e = threadIdx.x + NTH * k, r = e / NQ, d = 4 * (e % NQ);
+      int c, h;
+      if (e >= items || !real_row(e, c, h)) continue;
+      const float M = row_max(r);
+      float Z = merge_weight(s_sink[r], M);
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < TGW; ++w) {
@@ -736,8 +756,10 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
         o.w += x.w;
       }
       if (whole) {
-        const int64_t at = (((int64_t)b * a.C + c) * a.Hq + g * a.G + h) * HDIM + d0 + d;
-        paged_store4(o, Z, v_scale, a.gate ? a.gate + at : nullptr, a.out + at);
+        const int64_t at = out_at(e, c, h, d0);
+        uint2 gate = gates[EARLY ? k : 0];
+        if (!EARLY && a.gate) gate = *(const uint2*)(a.gate + at);
+        paged_store4(o, Z, v_scale, a.gate != nullptr, gate, a.out + at);
       } else {
         const int64_t row = (int64_t)blockIdx.x * ROWS + r;
         *(float4*)(a.part_o + row * HDIM + d0 + d) = o;
@@ -763,7 +785,7 @@ __global__ __launch_bounds__(NTP) void k_paged_merge(PagedAttnArgs a) {
   const int r = blockIdx.x * RPG + team / SG, part = team % SG;
   const bool real = r < a.C * a.G;
   const int c = real ? r / a.G : 0, h = real ? r % a.G : 0;
-  const int64_t row0 = (int64_t)items.x * a.part_rows + c * a.Gp + h;
+  const int64_t row0 = (int64_t)items.x * a.part_rows + (c << a.gp_shift) + h;
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   constexpr int U = 4;
@@ -829,7 +851,8 @@ __global__ __launch_bounds__(NTP) void k_paged_merge(PagedAttnArgs a) {
     o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
   }
   const int64_t at = (((int64_t)b * a.C + c) * a.Hq + g * a.G + h) * HDIM + 4 * dq;
-  paged_store4(o, l, a.v_scale ? a.v_scale[g] : 1.f, a.gate ? a.gate + at : nullptr, a.out + at);
+  const uint2 gate = a.gate ? *(const uint2*)(a.gate + at) : make_uint2(0, 0);
+  paged_store4(o, l, a.v_scale ? a.v_scale[g] : 1.f, a.gate != nullptr, gate, a.out + at);
 }
 
 // ============================================================================ append
@@ -896,8 +919,7 @@ __global__ __launch_bounds__(NTP) void k_paged_append(PagedAppendArgs a) {
 // ============================================================================ page operators
 // Sums over a workgroup's threads (sh: a word per wave; free again on return).
 __device__ inline int block_sum(int v, int* sh) {
-#pragma unroll
-  for (int w = 1; w < 64; w *= 2) v += __shfl_xor(v, w);
+  v = wave_sum(v);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
   int s = 0;
@@ -975,8 +997,7 @@ __global__ __launch_bounds__(NTP) void k_pages_scan(PagesArgs a) {
     const int32_t* row = a.table + (int64_t)b * a.max_pages;
     for (int j = threadIdx.x; j < a.max_pages; j += NTP)
       if (is_page(row[j], a.n_pages)) have = j + 1;
-#pragma unroll
-    for (int w = 1; w < 64; w *= 2) have = max(have, __shfl_xor(have, w));
+    have = wave_max(have);
     if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = have;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -993,8 +1014,7 @@ __global__ __launch_bounds__(NTP) void k_pages_scan(PagesArgs a) {
       if (pj == p) heir = min(heir, j);
       child |= pj == b;
     }
-#pragma unroll
-    for (int w = 1; w < 64; w *= 2) heir = min(heir, __shfl_xor(heir, w));
+    heir = a.B - wave_max(a.B - heir);
     if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = heir;
     child = __syncthreads_or(child);
     if (threadIdx.x == 0) {
@@ -1031,12 +1051,7 @@ __device__ inline PagesPlace pages_place(const PagesArgs& a, int b, int* pre, in
   int own = 0;
   for (int c = c0; c < min(c0 + per, a.n_chunks); ++c) own += a.chunk_n[c];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int incl = own;
-#pragma unroll
-  for (int w = 1; w < 64; w *= 2) {
-    const int x = __shfl_up(incl, w);
-    if (lane >= w) incl += x;
-  }
+  const int incl = wave_scan(own);
   if (lane == 63) sh[wave] = incl;
   __syncthreads();
   int base = incl - own;

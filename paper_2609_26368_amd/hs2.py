@@ -382,7 +382,7 @@ _F32 = (torch.float32,)
 # and word their refusal only when there is one (a call of the attention took
 # the host 9.2 us with _expect, of an append 10.5).
 def _current():
-    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else torch.cuda.current_device()
+    return torch._C._cuda_getDevice()
 
 
 def _take(t, name, shape, dtypes, index):
