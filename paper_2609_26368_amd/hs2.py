@@ -464,13 +464,22 @@ def hs2_paged_window_attn_fp8(dims, q, K8, V8, k_scale, v_scale, table, len, win
     _paged_attn(dims, q, K8, V8, (k_scale, v_scale), table, len, (window, first), sink, gate, out, workspace, stream)
 
 
+def _row_strides(t):
+    """Strides, 0 for extents of one (torch leaves any value there)."""
+    return tuple(s if n > 1 else 0 for n, s in zip(t.shape, t.stride()))
+
+
 def _paged_append(dims, k_new, v_new, n_new, scales, table, len, K, V, stream):
     index = _current()
     B, Hkv, D = dims.batch, dims.n_kv_heads, dims.head_dim
     shape, strides = k_new.shape, k_new.stride()
     if k_new.dim() != 4 or (shape[0], shape[2], shape[3]) != (B, Hkv, D) or shape[1] < 1:
         raise ValueError(f"k_new: shape {tuple(shape)}, expected ({B}, tokens, {Hkv}, {D})")
-    if v_new.shape != shape or v_new.stride() != strides or strides[3] != 1:
+    if v_new.stride() != strides or (strides[0] | strides[1] | strides[2]) & 7:
+        strides, v_strides = _row_strides(k_new), _row_strides(v_new)
+    else:
+        v_strides = strides
+    if v_new.shape != shape or v_strides != strides or strides[3] != 1:
         raise ValueError("k_new and v_new: one shape and one set of strides, rows of contiguous elements expected")
     for name, t in (("k_new", k_new), ("v_new", v_new)):
         if t.dtype not in _BF16 or t.get_device() != index:

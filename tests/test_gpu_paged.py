@@ -366,6 +366,43 @@ def test_append(kv, D, T, ragged, layout):
         assert torch.equal(bits(X.cpu()), bits(Y))
 
 
+def test_append_of_one_token_and_one_sequence_has_any_stride():
+    """Extents of one carry any stride."""
+    s = Setup(31, "bf16", 128, 2, 16, [33], layout="record", poison=False)
+    raw = torch.randn(2, 2, 128, device="cuda").to(torch.bfloat16)
+    k, v = torch.as_strided(raw[0], (1, 1, 2, 128), (3, 5, 128, 1)), raw[1].view(1, 1, 2, 128)
+    hs2.hs2_paged_append(s.dims(1, 2), k, v, None, s.dtable, s.dlen, s.K, s.V)
+    p = int(s.table[0, 2])
+    assert torch.equal(s.K[p, :, 0], raw[0]) and torch.equal(s.V[p, :, 0], raw[1])
+    with pytest.raises(hs2.HS2Error):
+        wide = torch.zeros(1, 2, 2, 132, dtype=torch.bfloat16, device="cuda")[..., :128]
+        hs2.hs2_paged_append(s.dims(1, 2), wide, wide, None, s.dtable, s.dlen, s.K, s.V)
+
+
+def test_binding_refusals():
+    s = Setup(32, "bf16", 128, 2, 16, [33, 7], layout="record")
+    q, sink, gate = s.queries(1, 8, True)
+    out, d = torch.empty_like(q), s.dims(1, 8)
+    ws = torch.empty(hs2.hs2_paged_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+
+    def call(**kw):
+        a = dict(q=q, K=s.K, V=s.V, table=s.dtable, len=s.dlen, sink=sink, gate=gate, out=out, ws=ws)
+        a.update(kw)
+        hs2.hs2_paged_attn(d, *a.values())
+    call()
+    for bad in (dict(q=q.float()), dict(q=q.cpu()), dict(q=q[:1]), dict(q=q.transpose(2, 3)), dict(K=s.K[:-1, :1, :1].clone()),
+                dict(V=s.V.view(torch.float16)), dict(table=s.dtable.long()), dict(table=s.dtable[:, :-1]),
+                dict(len=s.dlen.cpu()), dict(sink=sink[:-1]), dict(sink=sink.double()), dict(gate=gate[..., :64]),
+                dict(out=out.transpose(0, 1)), dict(ws=None), dict(ws=ws[::2])):
+        with pytest.raises(ValueError):
+            call(**bad)
+    with pytest.raises(hs2.HS2Error) as e:
+        call(ws=ws[:0])
+    assert e.value.status == hs2.HS2_ERR_WORKSPACE or e.value.status == hs2.HS2_ERR_NULL
+    with pytest.raises(hs2.HS2Error):
+        hs2.hs2_paged_window_attn(d, q, s.K, s.V, s.dtable, s.dlen, 0, 0, None, None, out, ws)
+
+
 @pytest.mark.parametrize("scale", [1.0, 0.0123, 1 / 3, 7.7e-3, 3.0e5, 1e-30])
 def test_every_bf16_value_to_e4m3(scale):
     """All 65536 bit patterns: ties, subnormals, saturation, infinities, NaN."""
