@@ -1156,20 +1156,34 @@ __global__ __launch_bounds__(NTP) void k_pages_reorder(PagesArgs a) {
 // grid (chunks): with n_used pages in use, the free pages before n_used are
 // the holes, the used ones from n_used on move there, rank by rank.  list[p]:
 // the rank of a page that moves, -2 for a hole, -1 for any other page.
+// ALONE: small pools, whose pages every workgroup counts itself, without a launch
+// before this one.
+template <bool ALONE>
 __global__ __launch_bounds__(NTP) void k_pages_list(PagesArgs a) {
   __shared__ int sh[NTP / 64];
   const int chunk = blockIdx.x;
   int before = 0, n_used = 0;
-  for (int c = threadIdx.x; c < a.n_chunks; c += NTP) {
-    const int n = a.chunk_n[c];
-    n_used += n;
-    if (c < chunk) before += n;
+  if constexpr (ALONE) {
+#pragma unroll 8
+    for (int p = threadIdx.x; p < a.n_pages; p += NTP) {
+      const int used = a.refs[p] > 0;
+      n_used += used;
+      if (p < chunk * PAGES_CHUNK) before += used;
+    }
+  } else {
+    for (int c = threadIdx.x; c < a.n_chunks; c += NTP) {
+      const int n = a.chunk_n[c];
+      n_used += n;
+      if (c < chunk) before += n;
+    }
   }
   before = block_sum(before, sh);
   n_used = block_sum(n_used, sh);
   int stay = 0;  // used pages before n_used
-  const int c0 = n_used / PAGES_CHUNK;
-  for (int c = threadIdx.x; c < c0; c += NTP) stay += a.chunk_n[c];
+  const int c0 = ALONE ? 0 : n_used / PAGES_CHUNK;
+  if constexpr (!ALONE)
+    for (int c = threadIdx.x; c < c0; c += NTP) stay += a.chunk_n[c];
+#pragma unroll 8
   for (int p = c0 * PAGES_CHUNK + threadIdx.x; p < n_used; p += NTP) stay += a.refs[p] > 0;
   stay = block_sum(stay, sh);
   if (chunk == 0 && threadIdx.x == 0) {
@@ -1333,10 +1347,13 @@ hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// a compaction of at most so many chunks needs no launch that counts them
+constexpr int PAGES_ALONE = 4;
+
 hipError_t launch_pages_scan(const PagesArgs& a, PagesOp op, hipStream_t s) {
   if (op == PagesOp::extend) k_pages_scan<PagesOp::extend><<<a.n_chunks + a.B, NTP, 0, s>>>(a);
   if (op == PagesOp::reorder) k_pages_scan<PagesOp::reorder><<<a.n_chunks + a.B, NTP, 0, s>>>(a);
-  if (op == PagesOp::compact) k_pages_scan<PagesOp::compact><<<a.n_chunks, NTP, 0, s>>>(a);
+  if (op == PagesOp::compact && a.n_chunks > PAGES_ALONE) k_pages_scan<PagesOp::compact><<<a.n_chunks, NTP, 0, s>>>(a);
   return hipGetLastError();
 }
 hipError_t launch_pages_extend(const PagesArgs& a, hipStream_t s) {
@@ -1348,7 +1365,10 @@ hipError_t launch_pages_reorder(const PagesArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 hipError_t launch_pages_list(const PagesArgs& a, hipStream_t s) {
-  k_pages_list<<<a.n_chunks, NTP, 0, s>>>(a);
+  if (a.n_chunks <= PAGES_ALONE)
+    k_pages_list<true><<<a.n_chunks, NTP, 0, s>>>(a);
+  else
+    k_pages_list<false><<<a.n_chunks, NTP, 0, s>>>(a);
   return hipGetLastError();
 }
 hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t s) {
