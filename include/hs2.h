@@ -293,9 +293,9 @@ hs2_status hs2_stream_read_probe(const void* src, size_t bytes, int32_t mode, ui
  *
  *   pool    K, V: element (p, g, s, d) of page p, KV head g, slot s at
  *           p*kv_stride_p + g*kv_stride_h + s*kv_stride_t + d (bf16, or E4M3
- *           bytes for the _fp8 entry points with scales as above; K and V
- *           share this layout; each token row is contiguous).  Several
- *           layers' pools may share one table.
+ *           bytes for the _fp8 entry points with scales as above, finite
+ *           and above 0; K and V share this layout; each token row is
+ *           contiguous).  Several layers' pools may share one table.
  *   table   [batch, max_pages] int32 (device): entry (b, j) is the page of
  *           sequence b's tokens j*page .. j*page + page - 1.  Entries outside
  *           [0, n_pages) are no page: reads skip their tokens (as if no query
@@ -357,7 +357,7 @@ hs2_status hs2_paged_window_attn_fp8(const hs2_paged_dims* dims, const uint16_t*
  *   k_new, v_new  bf16: row (b, i, g) at b*new_stride_b + i*new_stride_t +
  *           g*new_stride_h, D contiguous elements (strides multiples of 8,
  *           pointers 16-byte aligned), i in [0, n_tokens)
- *   n_tokens  >= 1 (dims->n_queries is not used)
+ *   n_tokens  >= 1, n_tokens * n_kv_heads < 2^27 (dims->n_queries is not used)
  *   n_new   [B] int32 (device) or NULL (n_tokens for every sequence): rows
  *           i < n_new[b] (clamped to [0, n_tokens]) are written, to token
  *           len[b] - n_new[b] + i; the rows behind them are not read.  Tokens

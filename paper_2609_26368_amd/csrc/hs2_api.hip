@@ -1151,8 +1151,9 @@ hs2_status paged_append_impl(const hs2_paged_dims* d, const uint16_t* k_new, con
                              void* K, void* V, void* stream) {
   hs2_status st = check_paged(d, kv8);
   if (st != HS2_OK) return st;
-  if (n_tokens < 1 || (int64_t)n_tokens * d->n_kv_heads > (1 << 27))
-    return fail(HS2_ERR_SHAPE, "n_tokens must be >= 1 and n_tokens * n_kv_heads at most 2^27 (got %d)", n_tokens);
+  // (the grid has at most 32 threads a row, and less than 2^32 of them)
+  if (n_tokens < 1 || (int64_t)n_tokens * d->n_kv_heads >= (1 << 27))
+    return fail(HS2_ERR_SHAPE, "n_tokens must be >= 1 and n_tokens * n_kv_heads below 2^27 (got %d)", n_tokens);
   if (!k_new || !v_new || !table || !len || !K || !V)
     return fail(HS2_ERR_NULL, "k_new, v_new, table, len, K and V are required");
   if (kv8 && (!k_scale || !v_scale)) return fail(HS2_ERR_NULL, "k_scale and v_scale are required for an FP8 cache");

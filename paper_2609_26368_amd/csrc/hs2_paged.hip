@@ -32,8 +32,11 @@ __device__ inline bool is_page(int id, int n_pages) { return (uint32_t)id < (uin
 // one pass over K and V with a running maximum and sum per query row:
 //   s_t = c2 <q, k_t>,  m' = max(m, s_t),  l' = l 2^(m - m') + 2^(s_t - m'),
 //   o' = o 2^(m - m') + 2^(s_t - m') v_t,  out = o / l   (c2 = scale log2 e).
-// Bound by reading K and V once: 4 G C operations a byte of a bf16 cache, far
-// below the matrix units' rate.
+// Bound by reading K and V once: G C operations a byte of a bf16 cache, far
+// below the matrix units' rate.  2 x 512K tokens (4.3 GB) 630 us, 6.8 TB/s; 64
+// sequences of 1000 to 12000 (1.7 GB) 271 us, 6.3 TB/s.  E4M3 with several row
+// tiles is bound by the vector work of the conversions (4 x 128K tokens, 64 rows
+// a KV head, 0.54 GB: 121 us, 4.4 TB/s).
 //
 // Tokens are taken in blocks of 16, which never straddle a page.  The blocks
 // that some query of the chunk sees are numbered through: nf blocks of first
@@ -772,7 +775,8 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
 }
 
 // Joins the splits' partial rows.  grid (row groups, B Hkv); NQ threads take a
-// row's column quads, SG such teams share a row's splits and meet in LDS.
+// row's column quads, SG such teams share a row's splits and meet in LDS.  Bound
+// by two memory latencies: 3.3 to 6.8 us.
 template <int HDIM, int SG>
 __global__ __launch_bounds__(NTP) void k_paged_merge(PagedAttnArgs a) {
   constexpr int NQ = HDIM / 4, TEAMS = NTP / NQ, RPG = TEAMS / SG;  // rows per workgroup
@@ -885,8 +889,8 @@ __device__ inline uint2 quantise8(const uint4& v, const E4m3Scale& k) {
 
 // grid (rows (token, KV head) / rows per workgroup, B); a thread takes 16
 // bytes of a K row and of its V row in the pool.  Bound by memory, E4M3 nearly as
-// much by the conversions: 8 x 4096 tokens of 8 heads (268 MB; E4M3 201) 30 us.
-// Several rows a thread were slower (2: 38 us, 4: 49).
+// much by the conversions: 8 x 4096 tokens of 8 heads (268 MB; E4M3 201) 30 us,
+// E4M3 24.  Several rows a thread were slower (2: 38 us, 4: 49).
 template <bool KV8, int HDIM>
 __global__ __launch_bounds__(NTP) void k_paged_append(PagedAppendArgs a) {
   constexpr int CPR = KV8 ? HDIM / 16 : HDIM / 8;  // 16-byte pieces of a pool row
@@ -1229,6 +1233,8 @@ __global__ __launch_bounds__(NTP) void k_pages_compact(PagesArgs a) {
 }
 
 // A workgroup copies the K and V rows of one KV head of one move at a time.
+// Bound by memory: 2000 pages (262 MB read, 262 written) 106 us, 5.0 TB/s; a
+// large library copy 5.2.
 __global__ __launch_bounds__(NTP) void k_pages_copy(PagesCopyArgs a) {
   const int cpr_shift = 31 - __clz(a.p.hd * a.esz / 16);  // 16-byte pieces of a row: a power of two
   const int n = min(max(a.n_moves[0], 0), a.max_moves);
@@ -1255,7 +1261,6 @@ __global__ __launch_bounds__(NTP) void k_pages_copy(PagesCopyArgs a) {
 // Shapes by query row tiles, cache format and head dim.  Columns: RT, E4M3, head
 // dim, row tiles per wave, waves per ring, token groups, rows and stages of a
 // ring.
-#ifndef HS2_PAGED_SHAPES
 #define HS2_PAGED_SHAPES(X)                                                        \
   X(1, false, 128, 1, 1, 4, 16, 2) X(2, false, 128, 2, 1, 4, 16, 2)          \
   X(4, false, 128, 2, 2, 2, 32, 2) X(8, false, 128, 2, 4, 1, 32, 2)          \
@@ -1265,7 +1270,6 @@ __global__ __launch_bounds__(NTP) void k_pages_copy(PagesCopyArgs a) {
   X(4, true, 128, 2, 2, 2, 32, 2) X(8, true, 128, 2, 4, 1, 32, 2)            \
   X(1, true, 256, 1, 1, 4, 16, 2) X(2, true, 256, 1, 2, 2, 32, 2)            \
   X(4, true, 256, 1, 4, 1, 32, 2) X(8, true, 256, 1, 8, 1, 32, 4)
-#endif
 
 PagedAttnShape paged_attn_shape(int RT, bool kv8, int hd) {
 #define HS2_PAGED_SHAPE(rt, f8, hdim, rpw, nwv, tgw, tw, ns)             \

@@ -669,7 +669,9 @@ class PagedCache:
     over every token (``window=``, ``first=``: over the recent and the first ones); ``reorder(parent)`` forks, permutes
     and frees sequences, ``compact()`` packs the pool.  With ``kv_scales=(k_scale, v_scale)`` the pool is E4M3.  No
     call waits for the device; the tensors ``K``, ``V``, ``table``, ``len`` and ``refs`` keep their addresses, so calls
-    can be captured in a graph.  ``counts`` holds what the last of extend, reorder and compact reported: counts[1] of
+    can be captured in a graph.  A sequence is not to grow past page * max_pages tokens (``len`` counts as that many,
+    and new rows go to the last of them), nor to shrink (a negative n) into a page that another one shares, which new
+    rows would change for both.  ``counts`` holds what the last of extend, reorder and compact reported: counts[1] of
     an extend or a reorder is the number of pages that the pool did not have.
     """
 

@@ -112,6 +112,7 @@ def test_other_refusals(lib):
     for name in ("hs2_paged_append", "hs2_paged_append_fp8"):
         assert call(lib, name, d, TOKENS=0) == S
         assert call(lib, name, d, TOKENS=1 << 26) == S
+        assert call(lib, name, d, TOKENS=(1 << 27) // d.n_kv_heads) == S
         for bad in (dict(SB=4), dict(ST=-8), dict(SH=12), dict(n_new=FAKE + 1)):
             assert call(lib, name, d, **bad) == A
     for name in ("hs2_paged_attn_fp8", "hs2_paged_window_attn_fp8", "hs2_paged_append_fp8"):  # 16-element strides
