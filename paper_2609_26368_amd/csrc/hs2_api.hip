@@ -1350,6 +1350,8 @@ hs2_status hs2_pages_copy(const hs2_paged_dims* d, const int32_t* moves, const i
   a.n_moves = n_moves;
   a.max_moves = max_moves;
   a.esz = elem_bytes;
+  // (a move reads and writes a page's K and V rows)
+  a.stream_moves = kLastLevelCacheBytes / 2 / (4ll * d->n_kv_heads * d->page * d->head_dim * elem_bytes);
   HS2_TRY_LAUNCH(KK_PAGES_COPY, (hipStream_t)stream, launch_pages_copy(a, (hipStream_t)stream));
   return HS2_OK;
 }

@@ -321,6 +321,7 @@ struct PagesCopyArgs {
   const int32_t* moves;
   const int32_t* n_moves;
   int max_moves, esz;
+  int64_t stream_moves;  // more moves than this go past the caches
 };
 hipError_t launch_pages_copy(const PagesCopyArgs& a, hipStream_t s);
 

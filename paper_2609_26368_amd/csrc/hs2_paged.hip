@@ -1160,36 +1160,45 @@ __global__ __launch_bounds__(NTP) void k_pages_reorder(PagesArgs a) {
 // grid (chunks): with n_used pages in use, the free pages before n_used are
 // the holes, the used ones from n_used on move there, rank by rank.  list[p]:
 // the rank of a page that moves, -2 for a hole, -1 for any other page.
-// ALONE: small pools, whose pages every workgroup counts itself, without a launch
-// before this one.
+// ALONE: pools of at most PAGES_ALONE chunks, whose pages every workgroup counts
+// itself, without a launch before this one: a bit each of every 256th.
+constexpr int PAGES_ALONE = 4;
 template <bool ALONE>
 __global__ __launch_bounds__(NTP) void k_pages_list(PagesArgs a) {
   __shared__ int sh[NTP / 64];
   const int chunk = blockIdx.x;
-  int before = 0, n_used = 0;
+  int before = 0, n_used = 0, stay = 0;  // used pages: before this chunk, all, before n_used
   if constexpr (ALONE) {
-#pragma unroll 8
-    for (int p = threadIdx.x; p < a.n_pages; p += NTP) {
-      const int used = a.refs[p] > 0;
-      n_used += used;
-      if (p < chunk * PAGES_CHUNK) before += used;
+    constexpr int PER = PAGES_CHUNK / NTP;
+    static_assert(PAGES_ALONE * PER <= 64 && PAGES_ALONE * PAGES_CHUNK < 1 << 15, "bits of a word, half a word a count");
+    unsigned long long bits = 0;
+    auto count = [&](int n) { return __popcll(n < 64 ? bits & ((1ull << n) - 1) : bits); };  // among the first n
+    for (int k0 = 0; k0 * NTP < a.n_pages; k0 += 2 * PER) {
+      int v[2 * PER];
+#pragma unroll
+      for (int k = 0; k < 2 * PER; ++k) v[k] = a.refs[min((k0 + k) * NTP + (int)threadIdx.x, a.n_pages - 1)];
+#pragma unroll
+      for (int k = 0; k < 2 * PER; ++k)
+        bits |= (unsigned long long)((k0 + k) * NTP + (int)threadIdx.x < a.n_pages && v[k] > 0) << (k0 + k);
     }
+    const int both = block_sum(__popcll(bits) << 16 | count(chunk * PER), sh);
+    before = both & 0xFFFF;
+    n_used = both >> 16;
+    stay = block_sum(count(max(0, n_used - (int)threadIdx.x + NTP - 1) / NTP), sh);
   } else {
     for (int c = threadIdx.x; c < a.n_chunks; c += NTP) {
       const int n = a.chunk_n[c];
       n_used += n;
       if (c < chunk) before += n;
     }
-  }
-  before = block_sum(before, sh);
-  n_used = block_sum(n_used, sh);
-  int stay = 0;  // used pages before n_used
-  const int c0 = ALONE ? 0 : n_used / PAGES_CHUNK;
-  if constexpr (!ALONE)
+    before = block_sum(before, sh);
+    n_used = block_sum(n_used, sh);
+    const int c0 = n_used / PAGES_CHUNK;
     for (int c = threadIdx.x; c < c0; c += NTP) stay += a.chunk_n[c];
 #pragma unroll 8
-  for (int p = c0 * PAGES_CHUNK + threadIdx.x; p < n_used; p += NTP) stay += a.refs[p] > 0;
-  stay = block_sum(stay, sh);
+    for (int p = c0 * PAGES_CHUNK + threadIdx.x; p < n_used; p += NTP) stay += a.refs[p] > 0;
+    stay = block_sum(stay, sh);
+  }
   if (chunk == 0 && threadIdx.x == 0) {
     a.counts[0] = n_used - stay;
     a.counts[1] = n_used;
@@ -1233,8 +1242,40 @@ __global__ __launch_bounds__(NTP) void k_pages_compact(PagesArgs a) {
 }
 
 // A workgroup copies the K and V rows of one KV head of one move at a time.
-// Bound by memory: 2000 pages (262 MB read, 262 written) 106 us, 5.0 TB/s; a
-// large library copy 5.2.
+// Bound by memory: 2000 pages (262 MB read, 262 written) 93 us, 5.6 TB/s; a large
+// library copy 5.2.  From stream_moves moves on, half the last-level cache's bytes,
+// nothing is kept there (123 MB moved 50.0 -> 43.8 us, 61 level, 31 17.7 -> 18.8).
+template <bool STREAM>
+__device__ inline void copy_rows(const PagesCopyArgs& a, int64_t src, int64_t dst, int pieces, int cpr_shift) {
+  constexpr int U = 2;  // rows of K and of V on their way (1: 105, 4: as 2, pages of 16 tokens slower by 4 %)
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  auto load = [](const unsigned char* p) {
+    return STREAM ? __builtin_nontemporal_load((const u32x4*)p) : *(const u32x4*)p;
+  };
+  auto store = [](u32x4 x, unsigned char* p) {
+    if (STREAM)
+      __builtin_nontemporal_store(x, (u32x4*)p);
+    else
+      *(u32x4*)p = x;
+  };
+  for (int i0 = threadIdx.x; i0 < pieces; i0 += NTP * U) {
+    u32x4 k[U], v[U];
+    int64_t off[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = min(i0 + u * NTP, pieces - 1);
+      off[u] = (i >> cpr_shift) * a.p.stride_t + 16 * (i & ((1 << cpr_shift) - 1));
+      k[u] = load(a.p.K + src + off[u]);
+      v[u] = load(a.p.V + src + off[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i0 + u * NTP < pieces) {
+        store(k[u], a.p.K + dst + off[u]);
+        store(v[u], a.p.V + dst + off[u]);
+      }
+  }
+}
 __global__ __launch_bounds__(NTP) void k_pages_copy(PagesCopyArgs a) {
   const int cpr_shift = 31 - __clz(a.p.hd * a.esz / 16);  // 16-byte pieces of a row: a power of two
   const int n = min(max(a.n_moves[0], 0), a.max_moves);
@@ -1246,12 +1287,10 @@ __global__ __launch_bounds__(NTP) void k_pages_copy(PagesCopyArgs a) {
     const int64_t head = (u % a.p.Hkv) * a.p.stride_h;
     const int64_t src = from * a.p.stride_p + head, dst = to * a.p.stride_p + head;
     const int pieces = tokens << cpr_shift;
-    for (int i = threadIdx.x; i < pieces; i += NTP) {
-      const int64_t off = (i >> cpr_shift) * a.p.stride_t + 16 * (i & ((1 << cpr_shift) - 1));
-      const uint4 k = *(const uint4*)(a.p.K + src + off), v = *(const uint4*)(a.p.V + src + off);
-      *(uint4*)(a.p.K + dst + off) = k;
-      *(uint4*)(a.p.V + dst + off) = v;
-    }
+    if (n > a.stream_moves)
+      copy_rows<true>(a, src, dst, pieces, cpr_shift);
+    else
+      copy_rows<false>(a, src, dst, pieces, cpr_shift);
   }
 }
 
@@ -1351,9 +1390,6 @@ hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// a compaction of at most so many chunks needs no launch that counts them
-constexpr int PAGES_ALONE = 4;
-
 hipError_t launch_pages_scan(const PagesArgs& a, PagesOp op, hipStream_t s) {
   if (op == PagesOp::extend) k_pages_scan<PagesOp::extend><<<a.n_chunks + a.B, NTP, 0, s>>>(a);
   if (op == PagesOp::reorder) k_pages_scan<PagesOp::reorder><<<a.n_chunks + a.B, NTP, 0, s>>>(a);
@@ -1383,7 +1419,8 @@ hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t s) {
 
 hipError_t launch_pages_copy(const PagesCopyArgs& a, hipStream_t s) {
   const int64_t n = (int64_t)a.max_moves * a.p.Hkv;
-  k_pages_copy<<<(unsigned)(n < 2048 ? n : 2048), NTP, 0, s>>>(a);
+  // (one unit a workgroup while the grid is small; 2048 107 us, 8192 103, 32768 the same)
+  k_pages_copy<<<(unsigned)(n < 8192 ? n : 8192), NTP, 0, s>>>(a);
   return hipGetLastError();
 }
 

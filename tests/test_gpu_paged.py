@@ -565,6 +565,29 @@ def test_copy(dtype, D, Hkv, page, layout):
             assert torch.equal(X.contiguous().view(torch.uint8), x)
 
 
+@pytest.mark.parametrize("dtype,P", [(torch.bfloat16, 80), (torch.uint8, 150)])
+def test_copy_past_the_caches(dtype, P):
+    """Moves on both sides of half the last-level cache (32 and 64 of these pages), pages of odd lengths among them."""
+    D, Hkv, page = 256, 8, 256
+    raw = torch.randint(0, 256, (P, Hkv, page, 2 * D * dtype.itemsize), dtype=torch.uint8, device="cuda").view(dtype)
+    K, V = raw[..., :D], raw[..., D:]
+    before = raw.view(torch.uint8).clone()
+    order = np.random.default_rng(P).permutation(P)
+    n = P // 2
+    tokens = np.full(n, page)
+    tokens[1], tokens[2], tokens[5], tokens[n - 1] = 0, 1, 37, 255
+    moves = np.stack([order[:n], order[n:2 * n], tokens], 1)
+    d = hs2.make_paged_dims(1, 1, Hkv, Hkv, D, page, P, 1, tuple(K.stride()[:3]))
+    m, = dev(moves)
+    edge = 32 if dtype == torch.bfloat16 else 64
+    for k in (edge, edge + 1, n):
+        hs2.hs2_pages_copy(d, m, torch.tensor([k], dtype=torch.int32, device="cuda"), K, V)
+        want = before.clone()
+        for a, e, t in moves[:k]:
+            want[e, :, :t] = want[a, :, :t]
+        assert torch.equal(raw.view(torch.uint8), want)
+
+
 # ------------------------------------------------------------------ together
 @pytest.mark.parametrize("kv", ["bf16", "e4m3"])
 @pytest.mark.parametrize("graph", [False, True])
