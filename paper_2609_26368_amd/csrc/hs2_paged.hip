@@ -21,6 +21,8 @@ namespace {
 
 constexpr int NTP = 256;  // threads per workgroup of this file's kernels
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 __device__ inline int paged_len(const PagedPool& p, int b) {
   const int L = p.len[b], cap = p.page * p.max_pages;
   return L < 0 ? 0 : (L > cap ? cap : L);
@@ -890,7 +892,8 @@ __device__ inline uint2 quantise8(const uint4& v, const E4m3Scale& k) {
 // grid (rows (token, KV head) / rows per workgroup, B); a thread takes 16
 // bytes of a K row and of its V row in the pool.  Bound by memory, E4M3 nearly as
 // much by the conversions: 8 x 4096 tokens of 8 heads (268 MB; E4M3 201) 30 us,
-// E4M3 24.  Several rows a thread were slower (2: 38 us, 4: 49).
+// E4M3 26.  Stored non-temporally (else 37 and 30 us; an attention that follows
+// takes what it did).  Several rows a thread were slower (2: 38 us, 4: 49).
 template <bool KV8, int HDIM>
 __global__ __launch_bounds__(NTP) void k_paged_append(PagedAppendArgs a) {
   constexpr int CPR = KV8 ? HDIM / 16 : HDIM / 8;  // 16-byte pieces of a pool row
@@ -904,19 +907,20 @@ __global__ __launch_bounds__(NTP) void k_paged_append(PagedAppendArgs a) {
   const int id = a.p.table[(int64_t)b * a.p.max_pages + (t >> a.p.page_shift)];
   const int64_t src = b * a.stride_b + i * a.stride_t + g * a.stride_h + piece * (KV8 ? 16 : 8);
   const int64_t dst = id * a.p.stride_p + g * a.p.stride_h + (t & (a.p.page - 1)) * a.p.stride_t + 16 * piece;
+  auto store = [](uint4 x, unsigned char* p) { __builtin_nontemporal_store(__builtin_bit_cast(u32x4, x), (u32x4*)p); };
   if constexpr (KV8) {
     const uint4 k0 = *(const uint4*)(a.k_new + src), k1 = *(const uint4*)(a.k_new + src + 8);
     const uint4 v0 = *(const uint4*)(a.v_new + src), v1 = *(const uint4*)(a.v_new + src + 8);
     if (!is_page(id, a.p.n_pages)) return;
     const E4m3Scale ks(a.k_scale[g]), vs(a.v_scale[g]);
     const uint2 ka = quantise8(k0, ks), kb = quantise8(k1, ks), va = quantise8(v0, vs), vb = quantise8(v1, vs);
-    *(uint4*)(a.p.K + dst) = make_uint4(ka.x, ka.y, kb.x, kb.y);
-    *(uint4*)(a.p.V + dst) = make_uint4(va.x, va.y, vb.x, vb.y);
+    store(make_uint4(ka.x, ka.y, kb.x, kb.y), a.p.K + dst);
+    store(make_uint4(va.x, va.y, vb.x, vb.y), a.p.V + dst);
   } else {
     const uint4 k = *(const uint4*)(a.k_new + src), v = *(const uint4*)(a.v_new + src);
     if (!is_page(id, a.p.n_pages)) return;
-    *(uint4*)(a.p.K + dst) = k;
-    *(uint4*)(a.p.V + dst) = v;
+    store(k, a.p.K + dst);
+    store(v, a.p.V + dst);
   }
 }
 
@@ -1248,7 +1252,6 @@ __global__ __launch_bounds__(NTP) void k_pages_compact(PagesArgs a) {
 template <bool STREAM>
 __device__ inline void copy_rows(const PagesCopyArgs& a, int64_t src, int64_t dst, int pieces, int cpr_shift) {
   constexpr int U = 2;  // rows of K and of V on their way (1: 105, 4: as 2, pages of 16 tokens slower by 4 %)
-  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
   auto load = [](const unsigned char* p) {
     return STREAM ? __builtin_nontemporal_load((const u32x4*)p) : *(const u32x4*)p;
   };
