@@ -1304,7 +1304,7 @@ __global__ __launch_bounds__(NTP) void k_pages_copy(PagesCopyArgs a) {
 // dim, row tiles per wave, waves per ring, token groups, rows and stages of a
 // ring.  Of one workgroup a compute unit (head dim 256), two groups of four waves
 // rather than one: another wave to each SIMD while one waits at its ring's barrier
-// (128 KV heads of 2000 tokens, 64 rows, E4M3 99 -> 78 us; bf16 63 -> 56); at head
+// (64 rows; 256 KV heads of 2000 tokens, E4M3 99 -> 78 us; 128 of 300 to 3000 63 -> 56); at head
 // dim 128, where two workgroups fit, 5 to 20 % slower.
 #define HS2_PAGED_SHAPES(X)                                                        \
   X(1, false, 128, 1, 1, 4, 16, 2) X(2, false, 128, 2, 1, 4, 16, 2)          \
