@@ -36,9 +36,9 @@ __device__ inline bool is_page(int id, int n_pages) { return (uint32_t)id < (uin
 //   o' = o 2^(m - m') + 2^(s_t - m') v_t,  out = o / l   (c2 = scale log2 e).
 // Bound by reading K and V once: G C operations a byte of a bf16 cache, far
 // below the matrix units' rate.  2 x 512K tokens (4.3 GB) 630 us, 6.8 TB/s; 64
-// sequences of 1000 to 12000 (1.7 GB) 271 us, 6.3 TB/s.  E4M3 with several row
+// sequences of 1000 to 12000 (1.7 GB) 271 to 280 us.  E4M3 with several row
 // tiles is bound by the vector work of the conversions (4 x 128K tokens, 64 rows
-// a KV head, 0.54 GB: 121 us, 4.4 TB/s).
+// a KV head, 0.54 GB: 121 to 128 us, 4.2 to 4.4 TB/s).
 //
 // Tokens are taken in blocks of 16, which never straddle a page.  The blocks
 // that some query of the chunk sees are numbered through: nf blocks of first
@@ -778,7 +778,7 @@ __global__ __launch_bounds__(64 * NWV * TGW) void k_paged_attn(PagedAttnArgs a) 
 
 // Joins the splits' partial rows.  grid (row groups, B Hkv); NQ threads take a
 // row's column quads, SG such teams share a row's splits and meet in LDS.  Bound
-// by two memory latencies: 3.3 to 6.8 us.
+// by two memory latencies: 3.5 to 7.0 us.
 template <int HDIM, int SG>
 __global__ __launch_bounds__(NTP) void k_paged_merge(PagedAttnArgs a) {
   constexpr int NQ = HDIM / 4, TEAMS = NTP / NQ, RPG = TEAMS / SG;  // rows per workgroup
@@ -1246,7 +1246,7 @@ __global__ __launch_bounds__(NTP) void k_pages_compact(PagesArgs a) {
 }
 
 // A workgroup copies the K and V rows of one KV head of one move at a time.
-// Bound by memory: 2000 pages (262 MB read, 262 written) 93 us, 5.6 TB/s; a large
+// Bound by memory: 2000 pages (262 MB read, 262 written) 94 us, 5.6 TB/s; a large
 // library copy 5.2.  From stream_moves moves on, half the last-level cache's bytes,
 // nothing is kept there (123 MB moved 50.0 -> 43.8 us, 61 level, 31 17.7 -> 18.8).
 template <bool STREAM>
